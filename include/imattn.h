@@ -263,6 +263,104 @@ int gsit_model_sizes(const im_shape_t* shape, const gsit_model_t* model, size_t*
 int gsit_model_fwd(const im_shape_t* shape, const gsit_model_t* model, const void* x, const int32_t* valid_len,
                    const uint8_t* key_pad, void* out, void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* ---- Operators around the attention of a layer, on tensors of the caller's own layout ----
+ *
+ * A head tensor [batch, rows, heads, head_dim] is a view: its first element and the distance, in ELEMENTS, from one
+ * batch element, row and head to the next; the head_dim elements of a head lie side by side.  Slices of one
+ * projection [B, T, 3 d] are views.  Pointers need their element's alignment; heads whose bytes, strides and
+ * first element are multiples of 16 are read and written in 16-byte units.  Strides of inputs may be 0
+ * (an input shared by batch elements or heads); an output's stride may be 0 only where there is one element to stride
+ * over.  Outputs must not overlap each other or an input, except where an entry point says so. */
+typedef struct im_view {
+  void* ptr;
+  int64_t batch, row, head;
+} im_view_t;
+
+/* Layer normalisation of rows of d elements, one row every ld* elements:
+ *   y = (x - mean) rstd gamma + beta,  mean = sum x / d,  rstd = 1 / sqrt(sum (x - mean)^2 / d + eps)
+ * and its gradients given dy:  w = dy gamma,  xhat = (x - mean) rstd,
+ *   dx = rstd (w - mean(w) - xhat mean(w xhat)),  dgamma = sum over rows of dy xhat,  dbeta = sum over rows of dy.
+ * device in : x, dy [rows, d]; gamma, beta [d] of the rows' dtype, or NULL (1 and 0); mean, rstd fp32 [rows] as the
+ *             forward wrote them.
+ * device out: y, dx [rows, d]; mean, rstd fp32 [rows], both or neither (NULL); dgamma, dbeta fp32 [d], overwritten,
+ *             each may be NULL, as may dx (not all three).  y may be x and dx may be dy (same pointer and ld).
+ * rows >= 0 (0: nothing is read, dgamma and dbeta become 0), 1 <= d <= IM_NORM_MAX_D, ld* >= d, eps finite and > 0.  Sums are
+ * held in fp32; results are bitwise reproducible.  workspace: of im_layernorm_sizes bytes, for im_layernorm_bwd. */
+#define IM_NORM_MAX_D 16384
+int im_layernorm_sizes(int64_t rows, int32_t d, int32_t dtype, size_t* workspace_bytes);
+int im_layernorm_fwd(int64_t rows, int32_t d, int32_t dtype, const void* x, int64_t ldx, const void* gamma, const void* beta,
+                     float eps, void* y, int64_t ldy, float* mean, float* rstd, void* hip_stream);
+int im_layernorm_bwd(int64_t rows, int32_t d, int32_t dtype, const void* x, int64_t ldx, const void* gamma, const float* mean,
+                     const float* rstd, const void* dy, int64_t lddy, void* dx, int64_t lddx, float* dgamma, float* dbeta,
+                     void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Rotary positions with several axes (time, height and width of a step): pair p of a head, which belongs to axis a,
+ * is turned by the angle pos[b, row, a] * inv_freq[p]:
+ *   (x0, x1) -> (x0 cos - x1 sin, x0 sin + x1 cos),  inverse: by the negative angle -- the gradient of the rotation.
+ * The first pairs[0] pairs belong to axis 0, the next pairs[1] to axis 1, ...; P = sum of pairs, 1 <= P <= head_dim / 2.
+ * Pair p is the elements (p, P + p) of a head, or (2p, 2p + 1) with `interleaved`; elements from 2P on are copied.
+ * Angles are formed and reduced in 64 bits: far positions lose nothing.
+ * device in : pos fp32 [batch, rows, n_axes], pos_batch elements from one batch element to the next (0: shared by all);
+ *             inv_freq fp32 [P]; views q (q_heads heads) and k (k_heads heads; 0: no keys, k and k_out may be NULL).
+ * device out: views q_out, k_out (may be q and k: in place, same strides).
+ * batch and rows may be 0. */
+#define IM_MAX_AXES 4
+typedef struct im_rotary {
+  int32_t batch, rows, n_axes, pairs[IM_MAX_AXES];
+  int32_t q_heads, k_heads, head_dim, interleaved, inverse, dtype;
+} im_rotary_t;
+int im_rotary_apply(const im_rotary_t* shape, const float* pos, int64_t pos_batch, const float* inv_freq, const im_view_t* q,
+                    const im_view_t* q_out, const im_view_t* k, const im_view_t* k_out, void* hip_stream);
+
+/* Attention of projected heads on the live blocks of an interlaced mask, with modified scores and further masks:
+ *   s(q, k) = scale <q, k>;   cap > 0:  s = cap tanh(s / cap);   slope given:  s = s - slope[head] |q_pos - k_pos|;
+ *   o(q) = sum over the keys that q sees of softmax(s) v,   lse(q) = log sum exp(s)  (natural logarithm).
+ * Query q of segment i sees key k of segment j iff bit (i * n_seg + j) of live_mask is set, k is no padding (valid_len, key_pad
+ * as in im_attention_fwd), q_doc = k_doc where documents are given, and, with `causal`, k_pos <= q_pos or
+ * k_pos < prefix[b] where a prefix is given.  A query that sees nothing has o = 0 and lse = -inf and
+ * contributes 0 to every gradient.  A key that no query sees may hold anything, also infinities and NaN.  Where a
+ * query sees a key or value that is not finite, its own results are unspecified (NaN as a rule); no other query's is touched, and in
+ * the backward no key's that none of those queries sees.
+ * n_heads is a multiple of n_kv_heads: query head h reads key head h / (n_heads / n_kv_heads).  Any head_dim from 1 to 128.
+ * Queries and keys have lengths of their own (q_len, k_len: segments one after the other; 0 is allowed, also for all).
+ * With few query rows (new tokens against a long cache) the keys are split over workgroups and the parts joined. */
+typedef struct im_core {
+  int32_t batch, n_seg;
+  int32_t q_len[IM_MAX_SEG], k_len[IM_MAX_SEG];
+  int32_t n_heads, n_kv_heads, head_dim;
+  uint64_t live_mask;
+  float scale; /* finite, >= 0 */
+  float cap;   /* 0: none; else 0.01 .. 1000 */
+  int32_t causal, dtype;
+} im_core_t;
+
+/* device arrays, each NULL where it is not used */
+typedef struct im_core_rules {
+  const int32_t* valid_len;    /* [batch, n_seg] valid keys of each key segment */
+  const uint8_t* key_pad;      /* [batch, Tk] != 0: padding */
+  const float *q_pos, *k_pos;  /* [batch, Tq], [batch, Tk] finite; needed with slope or causal */
+  const float* slope;          /* [n_heads] finite */
+  const float* prefix;         /* [batch]; needs causal */
+  const int32_t *q_doc, *k_doc; /* [batch, Tq], [batch, Tk]: both or neither */
+} im_core_rules_t;
+
+/* Bytes of the `saved` buffer (forward -> backward) and of the workspaces of the two calls (may be 0: NULL then). */
+int im_core_attention_sizes(const im_core_t* shape, size_t* saved_bytes, size_t* fwd_workspace_bytes, size_t* bwd_workspace_bytes);
+
+/* device in : views q [batch, Tq, n_heads, head_dim], k, v [batch, Tk, n_kv_heads, head_dim].
+ * device out: view o (as q); lse fp32 [batch, n_heads, Tq] or NULL; saved (opaque: o and the row statistics in fp32) or
+ *             NULL for inference. */
+int im_core_attention_fwd(const im_core_t* shape, const im_core_rules_t* rules, const im_view_t* q, const im_view_t* k,
+                          const im_view_t* v, const im_view_t* o, float* lse, void* saved, void* workspace,
+                          size_t workspace_bytes, void* hip_stream);
+
+/* Gradients given d_o (as o) and `saved` of the forward with the same arguments; dq, dk, dv overwritten (dk, dv: summed over
+ * the query heads of a key head); dslope fp32 [n_heads] or NULL, overwritten.  Bitwise reproducible. */
+int im_core_attention_bwd(const im_core_t* shape, const im_core_rules_t* rules, const im_view_t* q, const im_view_t* k,
+                          const im_view_t* v, const void* saved, const im_view_t* d_o, const im_view_t* dq,
+                          const im_view_t* dk, const im_view_t* dv, float* dslope, void* workspace, size_t workspace_bytes,
+                          void* hip_stream);
+
 /* Kernel timing for benchmarks (off by default).  While enabled, the library
  * brackets each kernel family it launches with hipEvents recorded on the call's
  * stream.  im_profile_get synchronises on the recorded events, so call it after

@@ -37,6 +37,30 @@ class ImWorkItem(C.Structure):
                 ("key_seg", C.c_int32 * IM_MAX_SEG), ("pairs", C.c_int64)]
 
 
+IM_MAX_AXES = 4
+IM_NORM_MAX_D = 16384
+
+
+class ImView(C.Structure):
+    _fields_ = [("ptr", C.c_void_p), ("batch", C.c_int64), ("row", C.c_int64), ("head", C.c_int64)]
+
+
+class ImRotary(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("rows", C.c_int32), ("n_axes", C.c_int32), ("pairs", C.c_int32 * IM_MAX_AXES),
+                ("q_heads", C.c_int32), ("k_heads", C.c_int32), ("head_dim", C.c_int32), ("interleaved", C.c_int32),
+                ("inverse", C.c_int32), ("dtype", C.c_int32)]
+
+
+class ImCore(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("n_seg", C.c_int32), ("q_len", C.c_int32 * IM_MAX_SEG), ("k_len", C.c_int32 * IM_MAX_SEG),
+                ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("live_mask", C.c_uint64),
+                ("scale", C.c_float), ("cap", C.c_float), ("causal", C.c_int32), ("dtype", C.c_int32)]
+
+
+class ImCoreRules(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("valid_len", "key_pad", "q_pos", "k_pos", "slope", "prefix", "q_doc", "k_doc")]
+
+
 class ImAttnError(RuntimeError):
     def __init__(self, code, msg):
         super().__init__(f"imattn error {code}: {msg}")
@@ -81,7 +105,17 @@ def lib():
         L.gsit_model_sizes.argtypes = [C.c_void_p, C.c_void_p, C.POINTER(C.c_size_t)]
         L.gsit_model_fwd.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                      C.c_size_t, C.c_void_p]
-        for f in (L.im_schedule_build, L.im_attention_sizes, L.im_attention_fwd, L.im_attention_bwd,
+        view, i32, i64 = C.POINTER(ImView), C.c_int32, C.c_int64
+        L.im_layernorm_sizes.argtypes = [i64, i32, i32, C.POINTER(sz)]
+        L.im_layernorm_fwd.argtypes = [i64, i32, i32, vp, i64, vp, vp, C.c_float, vp, i64, vp, vp, vp]
+        L.im_layernorm_bwd.argtypes = [i64, i32, i32, vp, i64, vp, vp, vp, vp, i64, vp, i64, vp, vp, vp, sz, vp]
+        L.im_rotary_apply.argtypes = [C.POINTER(ImRotary), vp, i64, vp] + [view] * 4 + [vp]
+        core, rules = C.POINTER(ImCore), C.POINTER(ImCoreRules)
+        L.im_core_attention_sizes.argtypes = [core] + [C.POINTER(sz)] * 3
+        L.im_core_attention_fwd.argtypes = [core, rules] + [view] * 4 + [vp, vp, vp, sz, vp]
+        L.im_core_attention_bwd.argtypes = [core, rules] + [view] * 3 + [vp] + [view] * 4 + [vp, vp, sz, vp]
+        for f in (L.im_layernorm_sizes, L.im_layernorm_fwd, L.im_layernorm_bwd, L.im_rotary_apply, L.im_core_attention_sizes,
+                  L.im_core_attention_fwd, L.im_core_attention_bwd, L.im_schedule_build, L.im_attention_sizes, L.im_attention_fwd, L.im_attention_bwd,
                   L.im_attention_fwd_noalloc, L.im_noalloc_init, L.im_calibrate_mfma, L.im_calibrate_copy,
                   L.gsit_layer_sizes, L.gsit_layer_fwd, L.gsit_model_sizes, L.gsit_model_fwd,
                   L.gsit_layer_train_sizes, L.gsit_layer_fwd_train, L.gsit_layer_bwd):
@@ -283,6 +317,228 @@ def gsit_model_fwd(shape, model, x, valid_len=None, key_pad=None, out=None, work
     _check(lib().gsit_model_fwd(C.byref(shape), C.byref(model), _p(x), _p(valid_len), _p(key_pad), _p(out),
                                 _p(workspace), wbytes, _stream()))
     return out
+
+
+# ---- operators around the attention of a layer ----
+
+_DTYPES = {torch.float32: IM_DTYPE_F32, torch.bfloat16: IM_DTYPE_BF16, "fp32": IM_DTYPE_F32, "bf16": IM_DTYPE_BF16}
+
+
+def _dtype(t):
+    if t not in _DTYPES:
+        raise ValueError(f"dtype must be float32 or bfloat16 (got {t})")
+    return _DTYPES[t]
+
+
+def _on_device(device, what, **tensors):
+    """The call goes to the current device's current stream: every tensor has to live on that device."""
+    if device.type != "cuda" or device.index != torch.cuda.current_device():
+        raise ValueError(f"{what}: tensors must be on the current GPU (cuda:{torch.cuda.current_device()}), got {device}")
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise ValueError(f"{what}: {name} is on {t.device}, not on {device}")
+
+
+def _want(what, name, t, shape, dtype, optional=False):
+    """A dense tensor of that shape and dtype; None only where it is optional."""
+    if t is None:
+        if optional:
+            return
+        raise ValueError(f"{what}: {name} is needed")
+    if t.shape != shape or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"{what}: {name} must be a contiguous {dtype} tensor of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)} "
+                         f"with strides {t.stride()}")
+
+
+def _want_bytes(what, name, t):
+    if t is None:
+        return None, 0
+    if t.dtype != torch.uint8 or not t.is_contiguous():
+        raise ValueError(f"{what}: {name} must be a contiguous uint8 tensor")
+    return C.c_void_p(t.data_ptr()), t.numel()
+
+
+def _rows(what, name, t, d, dtype, n=None):
+    """(rows, distance) of a tensor [..., d] whose rows lie at one distance from each other."""
+    if t.dim() < 1 or t.shape[-1] != d or t.dtype != dtype or (d > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{what}: {name} must be a {dtype} tensor [..., {d}] with its last dimension dense, got {t.dtype} {tuple(t.shape)} "
+                         f"with strides {t.stride()}")
+    rows, ld = 1, 0
+    for size, stride in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if size == 1:
+            continue
+        if rows == 1:
+            ld = stride
+        elif stride != ld * rows:
+            raise ValueError(f"{what}: the rows of {name} must lie at one distance from each other, got shape {tuple(t.shape)} with strides {t.stride()}")
+        rows *= size
+    if n is not None and rows != n:
+        raise ValueError(f"{what}: {name} has {rows} rows, {n} are needed")
+    return rows, ld if rows > 1 else d
+
+
+def im_layernorm_sizes(rows, d, dtype):
+    """Workspace bytes of im_layernorm_bwd."""
+    a = C.c_size_t(0)
+    _check(lib().im_layernorm_sizes(int(rows), int(d), _dtype(dtype), C.byref(a)))
+    return a.value
+
+
+def im_layernorm_fwd(x, gamma=None, beta=None, eps=1e-5, y=None, mean=None, rstd=None):
+    """y = layer norm of x [..., d] over its last dimension, rows at one distance.  mean, rstd: fp32 tensors with one element a
+    row that the backward needs, or None for inference.  y may be x."""
+    what = "im_layernorm_fwd"
+    y = torch.empty_like(x) if y is None else y
+    _on_device(x.device, what, gamma=gamma, beta=beta, y=y, mean=mean, rstd=rstd)
+    d = x.shape[-1]
+    rows, ldx = _rows(what, "x", x, d, x.dtype)
+    _, ldy = _rows(what, "y", y, d, x.dtype, rows)
+    for name, t in (("gamma", gamma), ("beta", beta)):
+        _want(what, name, t, (d,), x.dtype, True)
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        if t is not None:
+            _want(what, name, t.view(-1), (rows,), torch.float32)
+    _check(lib().im_layernorm_fwd(rows, d, _dtype(x.dtype), _p(x), ldx, _p(gamma), _p(beta), float(eps), _p(y), ldy, _p(mean), _p(rstd),
+                                  _stream()))
+    return y
+
+
+def im_layernorm_bwd(x, gamma, mean, rstd, dy, dx=None, dgamma=None, dbeta=None, workspace=None):
+    """Gradients of im_layernorm_fwd into those of dx [..., d], dgamma and dbeta (fp32 [d]) that are given.  dx may be dy."""
+    what = "im_layernorm_bwd"
+    _on_device(x.device, what, gamma=gamma, mean=mean, rstd=rstd, dy=dy, dx=dx, dgamma=dgamma, dbeta=dbeta, workspace=workspace)
+    d = x.shape[-1]
+    rows, ldx = _rows(what, "x", x, d, x.dtype)
+    _, lddy = _rows(what, "dy", dy, d, x.dtype, rows)
+    lddx = _rows(what, "dx", dx, d, x.dtype, rows)[1] if dx is not None else 0
+    _want(what, "gamma", gamma, (d,), x.dtype, True)
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        _want(what, name, t if t is None else t.view(-1), (rows,), torch.float32)
+    for name, t in (("dgamma", dgamma), ("dbeta", dbeta)):
+        _want(what, name, t, (d,), torch.float32, True)
+    ws, nbytes = _want_bytes(what, "workspace", workspace)
+    _check(lib().im_layernorm_bwd(rows, d, _dtype(x.dtype), _p(x), ldx, _p(gamma), _p(mean), _p(rstd), _p(dy), lddy, _p(dx), lddx, _p(dgamma),
+                                  _p(dbeta), ws, nbytes, _stream()))
+    return dx
+
+
+def _view(what, name, t, shape, dtype):
+    if t is None or t.shape != shape or t.dtype != dtype or (shape[3] > 1 and t.stride(3) != 1):
+        got = "None" if t is None else f"{t.dtype} {tuple(t.shape)} with strides {t.stride()}"
+        raise ValueError(f"{what}: {name} must be a {dtype} tensor of shape {tuple(shape)} with dense heads, got {got}")
+    return ImView(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+
+
+def im_rotary(pos, inv_freq, pairs, q, k=None, q_out=None, k_out=None, interleaved=False, inverse=False):
+    """Rotary positions on q [B, T, heads, head_dim] and, if given, k [B, T, k_heads, head_dim] (any strides, dense heads).
+    pos: fp32 [B, T, axes], or [T, axes] for all batch elements; pairs: rotated pairs of each axis; inv_freq: fp32
+    [sum of pairs].  inverse: the gradient's rotation.  q_out / k_out may be q / k.  Returns (q_out, k_out)."""
+    what = "im_rotary"
+    if q.dim() != 4 or (k is not None and k.dim() != 4):
+        raise ValueError(f"{what}: q and k must be [batch, rows, heads, head_dim]")
+    q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
+    if k is not None and k_out is None:
+        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    _on_device(q.device, what, pos=pos, inv_freq=inv_freq, k=k, q_out=q_out, k_out=k_out)
+    batch, rows, heads, dh = q.shape
+    pairs = [int(n) for n in pairs]
+    if not 1 <= len(pairs) <= IM_MAX_AXES:
+        raise ValueError(f"{what}: 1 to {IM_MAX_AXES} axes, got {len(pairs)}")
+    shared = pos.dim() == 2
+    _want(what, "pos", pos, (rows, len(pairs)) if shared else (batch, rows, len(pairs)), torch.float32)
+    _want(what, "inv_freq", inv_freq, (sum(pairs),), torch.float32)
+    s = ImRotary(batch, rows, len(pairs), (C.c_int32 * IM_MAX_AXES)(*pairs), heads, 0 if k is None else k.shape[2], dh, bool(interleaved),
+                 bool(inverse), _dtype(q.dtype))
+    views = [_view(what, "q", q, q.shape, q.dtype), _view(what, "q_out", q_out, q.shape, q.dtype)]
+    if k is not None:
+        shape = torch.Size((batch, rows, k.shape[2], dh))
+        views += [_view(what, "k", k, shape, q.dtype), _view(what, "k_out", k_out, shape, q.dtype)]
+    else:
+        views += [None, None]
+    _check(lib().im_rotary_apply(C.byref(s), _p(pos), 0 if shared else rows * len(pairs), _p(inv_freq), *views, _stream()))
+    return q_out, k_out
+
+
+def make_core(batch, q_len, k_len, n_heads, n_kv_heads, head_dim, live_mask, scale, dtype, cap=0.0, causal=False):
+    """The problem statement of im_core_attention_*: per-segment numbers of queries and keys, heads, block pattern, cap."""
+    s = ImCore()
+    if len(q_len) != len(k_len) or not 1 <= len(q_len) <= IM_MAX_SEG:
+        raise ValueError(f"q_len and k_len must have the same 1 to {IM_MAX_SEG} segments")
+    s.batch, s.n_seg, s.n_heads, s.n_kv_heads, s.head_dim = int(batch), len(q_len), int(n_heads), int(n_kv_heads), int(head_dim)
+    for i, (nq, nk) in enumerate(zip(q_len, k_len)):
+        s.q_len[i], s.k_len[i] = int(nq), int(nk)
+    s.live_mask, s.scale, s.cap, s.causal, s.dtype = int(live_mask), float(scale), float(cap), bool(causal), _dtype(dtype)
+    return s
+
+
+def im_core_attention_sizes(core):
+    """(saved bytes, forward workspace bytes, backward workspace bytes)"""
+    a, f, b = C.c_size_t(0), C.c_size_t(0), C.c_size_t(0)
+    _check(lib().im_core_attention_sizes(C.byref(core), C.byref(a), C.byref(f), C.byref(b)))
+    return a.value, f.value, b.value
+
+
+def _core_rules(what, core, shapes, rules):
+    """im_core_rules_t of the arrays that are given, their shapes checked."""
+    batch, tq, tk = shapes
+    want = {"valid_len": ((batch, core.n_seg), torch.int32), "key_pad": ((batch, tk), torch.uint8), "q_pos": ((batch, tq), torch.float32),
+            "k_pos": ((batch, tk), torch.float32), "slope": ((core.n_heads,), torch.float32), "prefix": ((batch,), torch.float32),
+            "q_doc": ((batch, tq), torch.int32), "k_doc": ((batch, tk), torch.int32)}
+    r = ImCoreRules()
+    for name, t in rules.items():
+        if t is not None:
+            _want(what, name, t, *want[name])
+            setattr(r, name, t.data_ptr())
+    return r
+
+
+def _core_shapes(core):
+    tq, tk = sum(core.q_len[:core.n_seg]), sum(core.k_len[:core.n_seg])
+    return torch.Size((core.batch, tq, core.n_heads, core.head_dim)), torch.Size((core.batch, tk, core.n_kv_heads, core.head_dim)), (core.batch, tq, tk)
+
+
+def im_core_attention_fwd(core, q, k, v, valid_len=None, key_pad=None, q_pos=None, k_pos=None, slope=None, prefix=None, q_doc=None,
+                          k_doc=None, o=None, lse=None, saved=None, workspace=None):
+    """o [B, Tq, heads, head_dim] = attention of q over k, v [B, Tk, kv_heads, head_dim] (any strides, dense heads) under the rules
+    given; see include/imattn.h.  lse: fp32 [B, heads, Tq] or None; saved / workspace: uint8 buffers of
+    im_core_attention_sizes (saved None for inference)."""
+    what = "im_core_attention_fwd"
+    if o is None:
+        o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    rules = dict(valid_len=valid_len, key_pad=key_pad, q_pos=q_pos, k_pos=k_pos, slope=slope, prefix=prefix, q_doc=q_doc, k_doc=k_doc)
+    _on_device(q.device, what, k=k, v=v, o=o, lse=lse, saved=saved, workspace=workspace, **rules)
+    shape_q, shape_k, n = _core_shapes(core)
+    r = _core_rules(what, core, n, rules)
+    dt = torch.bfloat16 if core.dtype == IM_DTYPE_BF16 else torch.float32
+    views = [_view(what, "q", q, shape_q, dt), _view(what, "k", k, shape_k, dt), _view(what, "v", v, shape_k, dt), _view(what, "o", o, shape_q, dt)]
+    _want(what, "lse", lse, (core.batch, core.n_heads, n[1]), torch.float32, True)
+    keep, have = _want_bytes(what, "saved", saved)
+    if saved is not None and have < im_core_attention_sizes(core)[0]:
+        raise ValueError(f"{what}: saved has {have} bytes, {im_core_attention_sizes(core)[0]} are needed")
+    ws, nbytes = _want_bytes(what, "workspace", workspace)
+    _check(lib().im_core_attention_fwd(C.byref(core), C.byref(r), *views, _p(lse), keep, ws, nbytes, _stream()))
+    return o
+
+
+def im_core_attention_bwd(core, q, k, v, saved, d_o, dq, dk, dv, dslope=None, valid_len=None, key_pad=None, q_pos=None, k_pos=None,
+                          slope=None, prefix=None, q_doc=None, k_doc=None, workspace=None):
+    """Gradients of im_core_attention_fwd with the same arguments and its `saved`: dq, dk, dv and, if given, dslope (fp32
+    [heads]) are overwritten."""
+    what = "im_core_attention_bwd"
+    rules = dict(valid_len=valid_len, key_pad=key_pad, q_pos=q_pos, k_pos=k_pos, slope=slope, prefix=prefix, q_doc=q_doc, k_doc=k_doc)
+    _on_device(q.device, what, k=k, v=v, saved=saved, d_o=d_o, dq=dq, dk=dk, dv=dv, dslope=dslope, workspace=workspace, **rules)
+    shape_q, shape_k, n = _core_shapes(core)
+    r = _core_rules(what, core, n, rules)
+    dt = torch.bfloat16 if core.dtype == IM_DTYPE_BF16 else torch.float32
+    views = [_view(what, m, t, shape_q if m in ("q", "d_o", "dq") else shape_k, dt)
+             for m, t in (("q", q), ("k", k), ("v", v), ("d_o", d_o), ("dq", dq), ("dk", dk), ("dv", dv))]
+    _want(what, "dslope", dslope, (core.n_heads,), torch.float32, True)
+    keep, have = _want_bytes(what, "saved", saved)
+    if saved is not None and have < im_core_attention_sizes(core)[0]:
+        raise ValueError(f"{what}: saved has {have} bytes, {im_core_attention_sizes(core)[0]} are needed")
+    ws, nbytes = _want_bytes(what, "workspace", workspace)
+    _check(lib().im_core_attention_bwd(C.byref(core), C.byref(r), *views[:3], keep, *views[3:], _p(dslope), ws, nbytes, _stream()))
+    return dq, dk, dv
 
 
 def im_calibrate_mfma(iters, sink):

@@ -12,7 +12,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SOURCES = ["api.hip", "attn_split.hip", "attn_tiny.hip", "gemm_alu.hip", "gemm_split.hip", "mfma_path.hip", "mfma_gemm.hip", "wgrad_ring.hip", "mfma_attn.hip", "mfma_attn_sub.hip",
-           "gsit_model.hip", "calibrate.hip"]
+           "gsit_model.hip", "calibrate.hip", "layernorm.hip", "rotary.hip", "core_attn.hip", "core_fwd_bf16.hip", "core_fwd_f32.hip",
+           "core_dq_bf16.hip", "core_dq_f32.hip", "core_dkv_bf16.hip", "core_dkv_f32.hip"]
 LIB = os.path.join(HERE, "libimattn.so")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Xclang", "-target-feature", "-Xclang",
          "-packed-fp32-ops", "-Wno-unused-command-line-argument", "-I", os.path.join(ROOT, "include"),

@@ -1,0 +1,299 @@
+// Entry points of the attention core: validation, launch shapes, workspaces, and the two small kernels that join the parts of
+// split keys and sum the slopes' gradients.  See include/imattn.h; the attention kernels are in core_attn_kernels.hpp.
+#include "core_attn.hpp"
+
+#include <math.h>
+#include <string.h>
+
+#include <algorithm>
+
+namespace imattn {
+
+// One wave a query row: o = sum over splits of 2^(m_s - m) o_s / sum of 2^(m_s - m) l_s.  Bound by latency: a few KB.
+template <class T>
+__global__ __launch_bounds__(256) void core_join_kernel(CoreArgs a) {
+  const long rows = (long)a.B * a.H * a.Tq, row = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  if (row >= rows) return;
+  float m = -3.402823466e38f;
+  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.part_ml[2 * (s * rows + row)]);
+  float l = 0.f, o0 = 0.f, o1 = 0.f;
+  for (int s = 0; s < a.splits; ++s) {
+    const long at = s * rows + row;
+    const float f = __builtin_amdgcn_exp2f(a.part_ml[2 * at] - m);
+    l += f * a.part_ml[2 * at + 1];
+    if (lane < a.dh) o0 += f * a.part_o[at * a.dh + lane];
+    if (lane + 64 < a.dh) o1 += f * a.part_o[at * a.dh + lane + 64];
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l, lse2 = m + log2f(l);
+  const long bh = row / a.Tq, t = row - bh * a.Tq, b = bh / a.H, head = bh - b * a.H;
+  T* o = (T*)a.o.ptr + b * a.o.batch + t * a.o.row + head * a.o.head;
+  if (lane < a.dh) stf(o + lane, o0 * inv);
+  if (lane + 64 < a.dh) stf(o + lane + 64, o1 * inv);
+  if (a.o32) {
+    if (lane < a.dh) a.o32[row * a.dh + lane] = o0 * inv;
+    if (lane + 64 < a.dh) a.o32[row * a.dh + lane + 64] = o1 * inv;
+  }
+  if (lane == 0) {
+    if (a.lse) a.lse[row] = lse2 * 0.69314718055994530942f;
+    if (a.lse2) a.lse2[row] = lse2;
+  }
+}
+
+// dslope[h] = sum over batch elements and rows of the rows' parts, one workgroup a head, in a fixed order, in fp64
+__global__ __launch_bounds__(1024) void core_dslope_kernel(const float* __restrict__ rows, int B, int H, int Tq, float* dslope) {
+  __shared__ double sums[1024];
+  const int h = blockIdx.x;
+  double s = 0.0;
+  for (int b = 0; b < B; ++b) {
+    const float* r = rows + ((long)b * H + h) * Tq;
+#pragma unroll 4
+    for (int t = threadIdx.x; t < Tq; t += 1024) s += r[t];
+  }
+  sums[threadIdx.x] = s;
+  __syncthreads();
+  for (int o = 512; o > 0; o >>= 1) {
+    if ((int)threadIdx.x < o) sums[threadIdx.x] += sums[threadIdx.x + o];
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) dslope[h] = (float)sums[0];
+}
+
+struct CoreLaunch {
+  bool few;
+  int tiles, splits;
+  unsigned grid;
+};
+
+static long seg_tiles(int n, int own) { return ((long)n + own - 1) / own; }
+
+// Shape of a launch that owns query rows (or key rows), and the owned segments in launch order.
+// few: four waves to 32 rows instead of 128 -- where 128 rows a workgroup would leave CUs idle or half of the rows empty.
+// splits (forward with few): until 4 workgroups a CU, each with at least 16 tiles of 32 keys.
+static CoreLaunch core_launch(const im_core_t* s, bool own_keys, bool may_split, CoreArgs* a) {
+  CoreLaunch L = {};
+  const int G = own_keys ? 1 : s->n_heads / s->n_kv_heads;
+  const int32_t* own_len = own_keys ? s->k_len : s->q_len;
+  const int32_t* other_len = own_keys ? s->q_len : s->k_len;
+  const long groups = (long)s->batch * s->n_kv_heads;
+  long t128 = 0, t32 = 0, most = 0;
+  long work[IM_MAX_SEG];
+  for (int i = 0; i < s->n_seg; ++i) {
+    t128 += seg_tiles(own_len[i] * G, 128);
+    t32 += seg_tiles(own_len[i] * G, 32);
+    work[i] = 0;
+    for (int j = 0; j < s->n_seg; ++j) {
+      const int bit = own_keys ? j * s->n_seg + i : i * s->n_seg + j;
+      if ((s->live_mask >> bit) & 1ull) work[i] += other_len[j];
+    }
+    most = std::max(most, work[i]);
+  }
+  L.few = t128 * groups < cu_count() || 4 * t128 > 2 * t32;
+  const int own = L.few ? 32 : 128;
+  L.tiles = (int)(L.few ? t32 : t128);
+  L.splits = 1;
+  if (may_split && L.few && L.tiles > 0) {
+    const long wgs = L.tiles * groups;
+    L.splits = (int)std::max<long>(1, std::min<long>((4l * cu_count() + wgs - 1) / wgs, most / (16 * 32)));
+  }
+  const long grid = (long)L.tiles * groups * L.splits;
+  L.grid = grid < (1l << 24) ? (unsigned)grid : 0xffffffffu;
+  if (a) {
+    int n = s->n_seg;
+    for (int i = 0; i < n; ++i) a->order[i] = i;
+    std::stable_sort(a->order, a->order + n, [&](int x, int y) { return work[x] > work[y]; });
+    a->tile_prefix[0] = 0;
+    for (int k = 0; k < n; ++k) a->tile_prefix[k + 1] = a->tile_prefix[k] + (int)seg_tiles(own_len[a->order[k]] * G, own);
+    a->splits = L.splits;
+  }
+  return L;
+}
+
+static int core_check(const char* what, const im_core_t* s) {
+  if (!s) return refuse(IM_ERR_INVALID, "%s: shape is NULL", what);
+  if (s->dtype != IM_DTYPE_F32 && s->dtype != IM_DTYPE_BF16) return refuse(IM_ERR_INVALID, "%s: dtype must be IM_DTYPE_F32 or IM_DTYPE_BF16 (got %d)", what, s->dtype);
+  if (s->batch < 1 || s->batch > 65535) return refuse(IM_ERR_INVALID, "%s: batch must be in 1..65535 (got %d)", what, s->batch);
+  if (s->n_seg < 1 || s->n_seg > IM_MAX_SEG) return refuse(IM_ERR_INVALID, "%s: n_seg must be in 1..%d (got %d)", what, IM_MAX_SEG, s->n_seg);
+  if (s->n_heads < 1 || s->n_heads > 65535 || s->n_kv_heads < 1 || s->n_heads % s->n_kv_heads)
+    return refuse(IM_ERR_INVALID, "%s: n_heads (%d) must be a positive multiple of n_kv_heads (%d)", what, s->n_heads, s->n_kv_heads);
+  if (s->head_dim < 1) return refuse(IM_ERR_INVALID, "%s: head_dim must be >= 1 (got %d)", what, s->head_dim);
+  if (s->head_dim > 128) return refuse(IM_ERR_UNSUPPORTED, "%s: head_dim must be <= 128 (got %d)", what, s->head_dim);
+  long tq = 0, tk = 0;
+  for (int i = 0; i < s->n_seg; ++i) {
+    if (s->q_len[i] < 0 || s->k_len[i] < 0) return refuse(IM_ERR_INVALID, "%s: q_len[%d] and k_len[%d] must be >= 0", what, i, i);
+    tq += s->q_len[i];
+    tk += s->k_len[i];
+  }
+  if (tq > (1 << 24) || tk > (1 << 24) || tq * (s->n_heads / s->n_kv_heads) > (1l << 30))
+    return refuse(IM_ERR_INVALID, "%s: too many rows (Tq = %ld, Tk = %ld; at most 2^24, and 2^30 query rows that share a key head)", what, tq, tk);
+  const int nb = s->n_seg * s->n_seg;
+  if (nb < 64 && (s->live_mask >> nb) != 0) return refuse(IM_ERR_INVALID, "%s: live_mask has bits set at or above n_seg^2 = %d", what, nb);
+  if (!(s->scale >= 0.f) || isinf(s->scale)) return refuse(IM_ERR_INVALID, "%s: scale must be finite and >= 0", what);
+  if (s->cap != 0.f && !(s->cap >= 0.01f && s->cap <= 1000.f)) return refuse(IM_ERR_INVALID, "%s: cap must be 0 or in 0.01..1000", what);
+  for (int own_keys = 0; own_keys < 2; ++own_keys)
+    if (core_launch(s, own_keys, !own_keys, nullptr).grid == 0xffffffffu)
+      return refuse(IM_ERR_INVALID, "%s: problem too large (2^24 workgroups or more)", what);
+  return IM_OK;
+}
+
+static int core_rules(const char* what, const im_core_t* s, const im_core_rules_t* r) {
+  const im_core_rules_t none = {};
+  if (!r) r = &none;
+  long tq = 0, tk = 0;
+  for (int i = 0; i < s->n_seg; ++i) { tq += s->q_len[i]; tk += s->k_len[i]; }
+  // arrays without an element may have no address
+  if ((r->slope || s->causal) && ((tq && !r->q_pos) || (tk && !r->k_pos))) return refuse(IM_ERR_INVALID, "%s: q_pos and k_pos are needed with slope or causal", what);
+  if (!s->causal && r->prefix) return refuse(IM_ERR_INVALID, "%s: prefix needs causal", what);
+  if (tq && tk && !r->q_doc != !r->k_doc) return refuse(IM_ERR_INVALID, "%s: q_doc and k_doc: both or neither", what);
+  const uintptr_t bits = (uintptr_t)r->valid_len | (uintptr_t)r->q_pos | (uintptr_t)r->k_pos | (uintptr_t)r->slope | (uintptr_t)r->prefix | (uintptr_t)r->q_doc |
+                         (uintptr_t)r->k_doc;
+  if (bits % 4) return refuse(IM_ERR_INVALID, "%s: an array of the rules is not aligned to its elements", what);
+  return IM_OK;
+}
+
+static void core_args(const im_core_t* s, const im_core_rules_t* r, CoreArgs* a) {
+  memset(a, 0, sizeof(*a));
+  a->B = s->batch; a->H = s->n_heads; a->Hkv = s->n_kv_heads; a->G = s->n_heads / s->n_kv_heads; a->dh = s->head_dim; a->n_seg = s->n_seg;
+  for (int i = 0; i < s->n_seg; ++i) {
+    a->q_off[i + 1] = a->q_off[i] + s->q_len[i];
+    a->k_off[i + 1] = a->k_off[i] + s->k_len[i];
+    for (int j = 0; j < s->n_seg; ++j)
+      if ((s->live_mask >> (i * s->n_seg + j)) & 1ull) { a->q_live[i] |= 1u << j; a->k_live[j] |= 1u << i; }
+  }
+  a->Tq = a->q_off[s->n_seg]; a->Tk = a->k_off[s->n_seg];
+  a->causal = s->causal != 0;
+  const bool bf = s->dtype == IM_DTYPE_BF16;
+  a->cap = s->cap;
+  a->cap2 = s->cap * 1.44269504088896340736f;
+  a->c_in = s->cap == 0.f ? s->scale * 1.44269504088896340736f : bf ? 2.f * 1.44269504088896340736f * s->scale / s->cap : s->scale / s->cap;
+  a->d_scale = s->cap != 0.f && bf ? 4.f * s->scale : s->scale;
+  if (r) {
+    a->valid_len = r->valid_len; a->key_pad = r->key_pad; a->slope = r->slope; a->prefix = r->prefix;
+    a->q_doc = r->q_doc; a->k_doc = r->k_doc;
+    if (r->slope || s->causal) { a->q_pos = r->q_pos; a->k_pos = r->k_pos; }
+  }
+}
+
+struct CoreSizes { size_t o32, saved, part_o, fwd, stat, bwd; };
+static CoreSizes core_sizes(const im_core_t* s) {
+  long tq = 0;
+  for (int i = 0; i < s->n_seg; ++i) tq += s->q_len[i];
+  const size_t rows = (size_t)s->batch * s->n_heads * tq;
+  CoreSizes z;
+  z.o32 = round256(rows * s->head_dim * 4);
+  z.saved = z.o32 + round256(rows * 4);
+  const int splits = core_launch(s, false, true, nullptr).splits;
+  z.part_o = splits > 1 ? round256(splits * rows * s->head_dim * 4) : 0;
+  z.fwd = splits > 1 ? z.part_o + round256(splits * rows * 8) : 0;
+  z.stat = round256(rows * 4);
+  z.bwd = 2 * z.stat;
+  return z;
+}
+
+static int check_buffer(const char* what, const char* name, const void* p, size_t have, size_t need) {
+  if (!need) return IM_OK;
+  if (!p || have < need) return refuse(IM_ERR_WORKSPACE, "%s: %s of %zu bytes, %zu needed", what, name, p ? have : (size_t)0, need);
+  if ((uintptr_t)p % 16) return refuse(IM_ERR_INVALID, "%s: %s must be 16-byte aligned", what, name);
+  return IM_OK;
+}
+
+}  // namespace imattn
+
+using namespace imattn;
+
+extern "C" {
+
+int im_core_attention_sizes(const im_core_t* shape, size_t* saved_bytes, size_t* fwd_workspace_bytes, size_t* bwd_workspace_bytes) {
+  if (int rc = core_check("im_core_attention_sizes", shape)) return rc;
+  const CoreSizes z = core_sizes(shape);
+  if (saved_bytes) *saved_bytes = z.saved;
+  if (fwd_workspace_bytes) *fwd_workspace_bytes = z.fwd;
+  if (bwd_workspace_bytes) *bwd_workspace_bytes = z.bwd;
+  return IM_OK;
+}
+
+int im_core_attention_fwd(const im_core_t* shape, const im_core_rules_t* rules, const im_view_t* q, const im_view_t* k,
+                          const im_view_t* v, const im_view_t* o, float* lse, void* saved, void* workspace,
+                          size_t workspace_bytes, void* hip_stream) {
+  const char* what = "im_core_attention_fwd";
+  if (int rc = core_check(what, shape)) return rc;
+  if (int rc = core_rules(what, shape, rules)) return rc;
+  CoreArgs a;
+  core_args(shape, rules, &a);
+  const bool bf = shape->dtype == IM_DTYPE_BF16;
+  const size_t es = bf ? 2 : 4;
+  const int64_t nq[3] = {a.B, a.Tq, a.H}, nk[3] = {a.B, a.Tk, a.Hkv};
+  if (int rc = check_view(what, "q", q, nq, es, false)) return rc;
+  if (int rc = check_view(what, "k", k, nk, es, false)) return rc;
+  if (int rc = check_view(what, "v", v, nk, es, false)) return rc;
+  if (int rc = check_view(what, "o", o, nq, es, true)) return rc;
+  if ((uintptr_t)lse % 4) return refuse(IM_ERR_INVALID, "%s: lse is not aligned to its elements", what);
+  if ((uintptr_t)saved % 16) return refuse(IM_ERR_INVALID, "%s: saved must be 16-byte aligned", what);
+  const CoreSizes z = core_sizes(shape);
+  if (int rc = check_buffer(what, "workspace", workspace, workspace_bytes, z.fwd)) return rc;
+  a.q = *q; a.k = *k; a.v = *v; a.o = *o; a.lse = lse;
+  a.vec = (view_in_16s(a.q, a.dh, es) ? VEC_Q : 0) | (view_in_16s(a.k, a.dh, es) ? VEC_K : 0) | (view_in_16s(a.v, a.dh, es) ? VEC_V : 0) |
+          (view_in_16s(a.o, a.dh, es) ? VEC_O : 0);
+  if (saved) { a.o32 = (float*)saved; a.lse2 = (float*)((char*)saved + z.o32); }
+  a.part_o = (float*)workspace; a.part_ml = (float*)((char*)workspace + z.part_o);
+  const CoreLaunch L = core_launch(shape, false, true, &a);
+  if (!L.grid) return IM_OK;
+  hipStream_t st = (hipStream_t)hip_stream;
+  ProfScope ps(PF_ATTN_FWD, st);
+  (bf ? launch_core_fwd_bf16 : launch_core_fwd_f32)(L.few, a, L.grid, st);
+  if (L.splits > 1) {
+    const dim3 grid((unsigned)(((long)a.B * a.H * a.Tq + 3) / 4));
+    if (bf) hipLaunchKernelGGL(core_join_kernel<bf16_t>, grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL(core_join_kernel<float>, grid, dim3(256), 0, st, a);
+  }
+  return after_launch(what);
+}
+
+int im_core_attention_bwd(const im_core_t* shape, const im_core_rules_t* rules, const im_view_t* q, const im_view_t* k,
+                          const im_view_t* v, const void* saved, const im_view_t* d_o, const im_view_t* dq,
+                          const im_view_t* dk, const im_view_t* dv, float* dslope, void* workspace, size_t workspace_bytes,
+                          void* hip_stream) {
+  const char* what = "im_core_attention_bwd";
+  if (int rc = core_check(what, shape)) return rc;
+  if (int rc = core_rules(what, shape, rules)) return rc;
+  CoreArgs a;
+  core_args(shape, rules, &a);
+  const bool bf = shape->dtype == IM_DTYPE_BF16;
+  const size_t es = bf ? 2 : 4;
+  const int64_t nq[3] = {a.B, a.Tq, a.H}, nk[3] = {a.B, a.Tk, a.Hkv};
+  if (int rc = check_view(what, "q", q, nq, es, false)) return rc;
+  if (int rc = check_view(what, "k", k, nk, es, false)) return rc;
+  if (int rc = check_view(what, "v", v, nk, es, false)) return rc;
+  if (int rc = check_view(what, "d_o", d_o, nq, es, false)) return rc;
+  if (int rc = check_view(what, "dq", dq, nq, es, true)) return rc;
+  if (int rc = check_view(what, "dk", dk, nk, es, true)) return rc;
+  if (int rc = check_view(what, "dv", dv, nk, es, true)) return rc;
+  if ((uintptr_t)dslope % 4) return refuse(IM_ERR_INVALID, "%s: dslope is not aligned to its elements", what);
+  if (dslope && !a.slope) return refuse(IM_ERR_INVALID, "%s: dslope without slope", what);
+  const CoreSizes z = core_sizes(shape);
+  if (z.saved && !saved) return refuse(IM_ERR_INVALID, "%s: saved is NULL", what);
+  if ((uintptr_t)saved % 16) return refuse(IM_ERR_INVALID, "%s: saved must be 16-byte aligned", what);
+  if (int rc = check_buffer(what, "workspace", workspace, workspace_bytes, z.bwd)) return rc;
+  a.q = *q; a.k = *k; a.v = *v; a.d_o = *d_o; a.dq = *dq; a.dk = *dk; a.dv = *dv;
+  a.vec = (view_in_16s(a.q, a.dh, es) ? VEC_Q : 0) | (view_in_16s(a.k, a.dh, es) ? VEC_K : 0) | (view_in_16s(a.v, a.dh, es) ? VEC_V : 0) |
+          (view_in_16s(a.d_o, a.dh, es) ? VEC_DO : 0) | (view_in_16s(a.dq, a.dh, es) ? VEC_DQ : 0) | (view_in_16s(a.dk, a.dh, es) ? VEC_DK : 0) |
+          (view_in_16s(a.dv, a.dh, es) ? VEC_DV : 0);
+  a.o32 = (float*)saved; a.lse2 = (float*)((char*)saved + z.o32);
+  a.delta = (float*)workspace;
+  a.dslope_rows = dslope ? (float*)((char*)workspace + z.stat) : nullptr;
+  hipStream_t st = (hipStream_t)hip_stream;
+  const CoreLaunch Lq = core_launch(shape, false, false, &a);
+  if (Lq.grid) {
+    ProfScope ps(PF_ATTN_DQ, st);
+    (bf ? launch_core_dq_bf16 : launch_core_dq_f32)(Lq.few, a, Lq.grid, st);
+  }
+  if (dslope) hipLaunchKernelGGL(core_dslope_kernel, dim3(a.H), dim3(1024), 0, st, a.dslope_rows, a.B, a.H, a.Tq, dslope);
+  const CoreLaunch Lk = core_launch(shape, true, false, &a);
+  if (Lk.grid) {
+    ProfScope ps(PF_ATTN_DKV, st);
+    (bf ? launch_core_dkv_bf16 : launch_core_dkv_f32)(Lk.few, a, Lk.grid, st);
+  }
+  return after_launch(what);
+}
+
+}  // extern "C"

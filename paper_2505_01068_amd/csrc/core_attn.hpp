@@ -1,0 +1,43 @@
+// Attention of projected heads with capped, biased and masked scores: host/device definitions (include/imattn.h).
+#pragma once
+#include "entry.hpp"
+
+namespace imattn {
+
+// One problem, passed to the kernels by value.  "Query row" below is a pair (position t, head g of the key head's group):
+// row t * G + g of a segment, so that the heads that share a key head share its tiles.
+struct CoreArgs {
+  int B, H, Hkv, G, dh, n_seg, Tq, Tk;
+  int q_off[IM_MAX_SEG + 1], k_off[IM_MAX_SEG + 1];
+  unsigned q_live[IM_MAX_SEG], k_live[IM_MAX_SEG];   // query segment -> live key segments, and back
+  // tiles of the kernel's own rows: segments in launch order, those with most to read first
+  int order[IM_MAX_SEG], tile_prefix[IM_MAX_SEG + 1];
+  int splits;                     // workgroups that share the keys of one tile (forward)
+  unsigned vec;                   // bit per tensor (VecBit): heads in aligned 16-byte units
+  int causal;
+  float c_in;                     // raw score -> argument of the cap (2 log2(e) scale / cap), or scale * log2(e) without one
+  float cap, cap2;                // cap and cap * log2(e)
+  float d_scale;                  // what the accumulated dQ, dK are multiplied by: scale (x 4 with the bf16 cap, see score())
+  im_view_t q, k, v, o, d_o, dq, dk, dv;
+  const int32_t* valid_len;
+  const uint8_t* key_pad;
+  const float *q_pos, *k_pos, *slope, *prefix;
+  const int32_t *q_doc, *k_doc;
+  float* lse;                     // [B, H, Tq], natural logarithm
+  float *o32, *lse2;              // saved: [B, H, Tq, dh] and [B, H, Tq] in log2
+  float *delta, *dslope_rows;     // [B, H, Tq]
+  float *part_o, *part_ml;        // [splits][B, H, Tq][dh], [splits][B, H, Tq][2]
+};
+enum VecBit { VEC_Q = 1, VEC_K = 2, VEC_V = 4, VEC_O = 8, VEC_DO = 16, VEC_DQ = 32, VEC_DK = 64, VEC_DV = 128 };
+
+enum CoreKernel { CORE_FWD = 0, CORE_DQ = 1, CORE_DKV = 2 };
+// Whether the workgroup's four waves take 32 rows each and share every streamed tile (false), or take the same 32 rows and a
+// quarter of the streamed tiles each (true).
+void launch_core_fwd_f32(bool few, const CoreArgs& a, unsigned grid, hipStream_t st);
+void launch_core_fwd_bf16(bool few, const CoreArgs& a, unsigned grid, hipStream_t st);
+void launch_core_dq_f32(bool few, const CoreArgs& a, unsigned grid, hipStream_t st);
+void launch_core_dq_bf16(bool few, const CoreArgs& a, unsigned grid, hipStream_t st);
+void launch_core_dkv_f32(bool few, const CoreArgs& a, unsigned grid, hipStream_t st);
+void launch_core_dkv_bf16(bool few, const CoreArgs& a, unsigned grid, hipStream_t st);
+
+}  // namespace imattn

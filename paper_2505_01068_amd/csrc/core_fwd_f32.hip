@@ -1,0 +1,8 @@
+// Instances of the attention core's forward kernel for fp32.
+#include "core_attn_kernels.hpp"
+
+namespace imattn {
+
+void launch_core_fwd_f32(bool few, const CoreArgs& a, unsigned grid, hipStream_t st) { core_widths<float, CORE_FWD>(few, a, grid, st); }
+
+}  // namespace imattn

@@ -1,0 +1,40 @@
+// Helpers of the entry points: error returns, a view's checks.
+#pragma once
+#include "common.hpp"
+
+namespace imattn {
+
+template <class... A>
+inline int refuse(int code, const char* fmt, A... a) {
+  set_error(fmt, a...);
+  return code;
+}
+
+inline int after_launch(const char* what) {
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? IM_OK : refuse(IM_ERR_HIP, "%s launch: %s", what, hipGetErrorString(e));
+}
+
+inline size_t round256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+// A view of `n[0]` batch elements, `n[1]` rows and `n[2]` heads; an output's elements must not share a place by a stride of 0.
+inline int check_view(const char* what, const char* name, const im_view_t* v, const int64_t (&n)[3], size_t es, bool output) {
+  if (!v) return refuse(IM_ERR_INVALID, "%s: %s is NULL", what, name);
+  if (n[0] == 0 || n[1] == 0 || n[2] == 0) return IM_OK;
+  if (!v->ptr) return refuse(IM_ERR_INVALID, "%s: %s has a NULL pointer", what, name);
+  if ((uintptr_t)v->ptr % es) return refuse(IM_ERR_INVALID, "%s: %s is not aligned to its elements", what, name);
+  const int64_t st[3] = {v->batch, v->row, v->head};
+  for (int i = 0; i < 3; ++i) {
+    if (n[i] == 1) continue;
+    if (st[i] < 0 || st[i] > (1ll << 40)) return refuse(IM_ERR_INVALID, "%s: %s has a stride outside 0..2^40", what, name);
+    if (output && st[i] == 0) return refuse(IM_ERR_INVALID, "%s: %s is written and has a stride of 0", what, name);
+  }
+  return IM_OK;
+}
+
+// whether every head of the view starts on 16 bytes and is whole 16-byte units long
+inline bool view_in_16s(const im_view_t& v, int head_dim, size_t es) {
+  return (uintptr_t)v.ptr % 16 == 0 && head_dim * es % 16 == 0 && v.batch * es % 16 == 0 && v.row * es % 16 == 0 && v.head * es % 16 == 0;
+}
+
+}  // namespace imattn
