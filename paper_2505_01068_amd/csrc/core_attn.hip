@@ -25,7 +25,7 @@ __global__ __launch_bounds__(256) void core_join_kernel(CoreArgs a) {
     if (lane < a.dh) o0 += f * a.part_o[at * a.dh + lane];
     if (lane + 64 < a.dh) o1 += f * a.part_o[at * a.dh + lane + 64];
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l, lse2 = m + log2f(l);
+  const float inv = l == 0.f ? 0.f : 1.f / l, lse2 = l == 0.f ? IM_NEG_INF : m + log2f(l);
   const long bh = row / a.Tq, t = row - bh * a.Tq, b = bh / a.H, head = bh - b * a.H;
   T* o = (T*)a.o.ptr + b * a.o.batch + t * a.o.row + head * a.o.head;
   if (lane < a.dh) stf(o + lane, o0 * inv);
@@ -162,17 +162,19 @@ static void core_args(const im_core_t* s, const im_core_rules_t* r, CoreArgs* a)
   }
   a->Tq = a->q_off[s->n_seg]; a->Tk = a->k_off[s->n_seg];
   a->causal = s->causal != 0;
-  const bool bf = s->dtype == IM_DTYPE_BF16;
   a->cap = s->cap;
   a->cap2 = s->cap * 1.44269504088896340736f;
-  a->c_in = s->cap == 0.f ? s->scale * 1.44269504088896340736f : bf ? 2.f * 1.44269504088896340736f * s->scale / s->cap : s->scale / s->cap;
-  a->d_scale = s->cap != 0.f && bf ? 4.f * s->scale : s->scale;
+  a->c_in = s->cap == 0.f ? s->scale * 1.44269504088896340736f : s->scale / s->cap;
+  a->scale = s->scale;
   if (r) {
     a->valid_len = r->valid_len; a->key_pad = r->key_pad; a->slope = r->slope; a->prefix = r->prefix;
     a->q_doc = r->q_doc; a->k_doc = r->k_doc;
     if (r->slope || s->causal) { a->q_pos = r->q_pos; a->k_pos = r->k_pos; }
   }
 }
+
+// Streamed tensors in 16-byte units are addressed by 32-bit byte offsets within a tile of up to 64 rows.
+static unsigned vec_bit(const im_view_t& v, int dh, size_t es, unsigned bit) { return view_in_16s(v, dh, es) && (uint64_t)v.row * es * 64 < (1ull << 32) ? bit : 0u; }
 
 struct CoreSizes { size_t o32, saved, part_o, fwd, stat, bwd; };
 static CoreSizes core_sizes(const im_core_t* s) {
@@ -232,8 +234,8 @@ int im_core_attention_fwd(const im_core_t* shape, const im_core_rules_t* rules, 
   const CoreSizes z = core_sizes(shape);
   if (int rc = check_buffer(what, "workspace", workspace, workspace_bytes, z.fwd)) return rc;
   a.q = *q; a.k = *k; a.v = *v; a.o = *o; a.lse = lse;
-  a.vec = (view_in_16s(a.q, a.dh, es) ? VEC_Q : 0) | (view_in_16s(a.k, a.dh, es) ? VEC_K : 0) | (view_in_16s(a.v, a.dh, es) ? VEC_V : 0) |
-          (view_in_16s(a.o, a.dh, es) ? VEC_O : 0);
+  a.vec = vec_bit(a.q, a.dh, es, VEC_Q) | vec_bit(a.k, a.dh, es, VEC_K) | vec_bit(a.v, a.dh, es, VEC_V) |
+          vec_bit(a.o, a.dh, es, VEC_O);
   if (saved) { a.o32 = (float*)saved; a.lse2 = (float*)((char*)saved + z.o32); }
   a.part_o = (float*)workspace; a.part_ml = (float*)((char*)workspace + z.part_o);
   const CoreLaunch L = core_launch(shape, false, true, &a);
@@ -275,9 +277,9 @@ int im_core_attention_bwd(const im_core_t* shape, const im_core_rules_t* rules, 
   if ((uintptr_t)saved % 16) return refuse(IM_ERR_INVALID, "%s: saved must be 16-byte aligned", what);
   if (int rc = check_buffer(what, "workspace", workspace, workspace_bytes, z.bwd)) return rc;
   a.q = *q; a.k = *k; a.v = *v; a.d_o = *d_o; a.dq = *dq; a.dk = *dk; a.dv = *dv;
-  a.vec = (view_in_16s(a.q, a.dh, es) ? VEC_Q : 0) | (view_in_16s(a.k, a.dh, es) ? VEC_K : 0) | (view_in_16s(a.v, a.dh, es) ? VEC_V : 0) |
-          (view_in_16s(a.d_o, a.dh, es) ? VEC_DO : 0) | (view_in_16s(a.dq, a.dh, es) ? VEC_DQ : 0) | (view_in_16s(a.dk, a.dh, es) ? VEC_DK : 0) |
-          (view_in_16s(a.dv, a.dh, es) ? VEC_DV : 0);
+  a.vec = vec_bit(a.q, a.dh, es, VEC_Q) | vec_bit(a.k, a.dh, es, VEC_K) | vec_bit(a.v, a.dh, es, VEC_V) |
+          vec_bit(a.d_o, a.dh, es, VEC_DO) | vec_bit(a.dq, a.dh, es, VEC_DQ) | vec_bit(a.dk, a.dh, es, VEC_DK) |
+          vec_bit(a.dv, a.dh, es, VEC_DV);
   a.o32 = (float*)saved; a.lse2 = (float*)((char*)saved + z.o32);
   a.delta = (float*)workspace;
   a.dslope_rows = dslope ? (float*)((char*)workspace + z.stat) : nullptr;

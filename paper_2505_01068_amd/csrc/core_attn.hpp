@@ -15,9 +15,9 @@ struct CoreArgs {
   int splits;                     // workgroups that share the keys of one tile (forward)
   unsigned vec;                   // bit per tensor (VecBit): heads in aligned 16-byte units
   int causal;
-  float c_in;                     // raw score -> argument of the cap (2 log2(e) scale / cap), or scale * log2(e) without one
+  float c_in;                     // raw score -> argument of the tangent (scale / cap), or scale * log2(e) without a cap
   float cap, cap2;                // cap and cap * log2(e)
-  float d_scale;                  // what the accumulated dQ, dK are multiplied by: scale (x 4 with the bf16 cap, see score())
+  float scale;
   im_view_t q, k, v, o, d_o, dq, dk, dv;
   const int32_t* valid_len;
   const uint8_t* key_pad;

@@ -35,6 +35,7 @@ constexpr int CORE_WAVES = 4;
 constexpr int CORE_LIST = 256;   // streamed tiles classified at a time
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 struct F8 { float v[8]; };
 template <class T> struct CoreT;
 template <> struct CoreT<bf16_t> { using Frag = bf16x8; static constexpr int EPC = 8; };
@@ -51,58 +52,89 @@ __device__ __forceinline__ f32x16 zero16() {
 __device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
 
 // ---- LDS tiles: ROWS rows of ND * 32 elements ----
-// bf16: panels of 64 columns, swizzled as lds_frag_sw expects.  fp32: rows of 32 ND floats, 16-byte unit c of row r at c ^ (r % 8).
+// bf16: panels of 64 columns, 8 units of 16 bytes a row, swizzled by sw_f.  fp32: rows of 32 ND floats, unit c of row r at c ^ (r % 8).
 template <class T, int ND, int ROWS>
 struct Tile {
-  static constexpr int CPR = ND * 32 / CoreT<T>::EPC;   // 16-byte units of a row
-  static constexpr int BYTES = sizeof(T) == 2 ? (ND + 1) / 2 * ROWS * 128 : ROWS * ND * 128;
-  static __device__ __forceinline__ int unit_at(int row, int c) {   // byte offset of unit c of a row
-    if constexpr (sizeof(T) == 2) return (c >> 3) * ROWS * 128 + row * 128 + (((c & 7) ^ sw_f(row & 15)) << 4);
-    else return row * ND * 128 + ((c ^ (row & 7)) << 4);
+  static constexpr bool BF = sizeof(T) == 2;
+  static constexpr int SLOTS = BF ? (ND + 1) / 2 * ROWS * 8 : ROWS * ND * 8;   // 16-byte units
+  static constexpr int BYTES = SLOTS * 16;
+  static constexpr int ROW = BF ? 128 : ND * 128;                              // bytes from row to row
+  // row and unit (of the row's data) that slot i of the tile holds
+  static __device__ __forceinline__ int row_of(int i) { return BF ? (i >> 3) % ROWS : i / (ND * 8); }
+  static __device__ __forceinline__ int unit_of(int i) {
+    if constexpr (BF) return ((i & 7) ^ sw_f(row_of(i))) + 8 * (i / (ROWS * 8));
+    else return (i % (ND * 8)) ^ (row_of(i) & 7);
   }
 };
 
-// operand by rows: streamed row (in the order perm32) lane % 32 of the 32-row block, contraction step s of 16 elements
-template <int ND, int ROWS>
-__device__ __forceinline__ bf16x8 row_frag(const bf16_t*, const char* tile, int row32, int s, int lane) {
-  const int lrow = perm32(lane & 31);
-  return lds_frag_sw((const bf16_t*)(tile + (s >> 2) * ROWS * 128), row32, lrow, 2 * (s & 3) + (lane >> 5));
+__device__ __forceinline__ unsigned lds_at(const void* p) { return (unsigned)(uintptr_t)p; }
+template <class V>
+__device__ __forceinline__ V lds_load(unsigned at, int off) {
+  typedef char __attribute__((address_space(3))) * lds_char_ptr;
+  typedef V __attribute__((address_space(3))) * lds_v_ptr;
+  return *(lds_v_ptr)((lds_char_ptr)at + off);
 }
-// fp32: elements 16 s + 4 h .. + 3 and 16 s + 8 + 4 h .. + 3, so that a head of up to 8 elements takes half a step
+
+// Where a lane reads its operands, as byte offsets into a tile.
+//   by rows: streamed row (in the order perm32) lane % 32 of a 32-row block.  bf16: elements 16 s + 8 h .. + 7 of step s.  fp32: 16 s +
+//   4 h .. + 3 and 16 s + 8 + 4 h .. + 3, so that a head of up to 8 elements takes half a step.
+//   by columns: column (in the order perm32) lane % 32 of a 32-column block, streamed rows 8 h .. + 7 of a 16-row block.
+template <class T, int ND, int ROWS>
+struct LaneAt;
 template <int ND, int ROWS>
-__device__ __forceinline__ F8 row_frag(const float*, const char* tile, int row32, int s, int lane) {
-  const int row = row32 + perm32(lane & 31), h = lane >> 5;
-  F8 f;
+struct LaneAt<bf16_t, ND, ROWS> {
+  using TL = Tile<bf16_t, ND, ROWS>;
+  unsigned row[ND == 1 ? 2 : 4], col[ND == 1 ? 1 : 2][2];
+  __device__ __forceinline__ LaneAt(int lane) {
+    const int r = perm32(lane & 31), h = lane >> 5;
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const float4 u = *(const float4*)(tile + Tile<float, ND, ROWS>::unit_at(row, 4 * s + 2 * i + h));
-    f.v[4 * i] = u.x; f.v[4 * i + 1] = u.y; f.v[4 * i + 2] = u.z; f.v[4 * i + 3] = u.w;
+    for (int j = 0; j < (ND == 1 ? 2 : 4); ++j) row[j] = r * 128 + (((2 * j + h) ^ sw_f(r)) << 4);
+    const int j = lane & 15, g = lane >> 4, lrow = 8 * (g >> 1) + (j >> 2), chunk = 2 * (g & 1) + (j & 1), f = sw_f(lrow);
+#pragma unroll
+    for (int m = 0; m < (ND == 1 ? 1 : 2); ++m) {   // the transpose read's lanes, blocks of four columns exchanged as lds_frag_tr_sw_perm does
+      col[m][0] = lrow * 128 + (((4 * m | chunk) ^ f) << 4) + 8 * ((j >> 1) & 1);
+      col[m][1] = (lrow + 4) * 128 + (((4 * m | chunk) ^ f ^ 1) << 4) + 8 * ((j >> 1) & 1);
+    }
   }
-  return f;
-}
-__device__ __forceinline__ f32x16 mma_rows(bf16x8 a, bf16x8 b, f32x16 c, int) { return mfma32(a, b, c); }
-__device__ __forceinline__ f32x16 mma_rows(const F8& a, const F8& b, f32x16 c, int left) {   // left: elements of the head from this step on
-#pragma unroll
-  for (int j = 0; j < 4; ++j) c = mfma_f32(a.v[j], b.v[j], c);
-  if (left > 8) {
-#pragma unroll
-    for (int j = 4; j < 8; ++j) c = mfma_f32(a.v[j], b.v[j], c);
+  __device__ __forceinline__ f32x16 rows(unsigned tile, int row32, int s, bf16x8 own, f32x16 c, int) const {
+    return mfma32(lds_load<bf16x8>(tile + row[s & 3], (s >> 2) * ROWS * 128 + row32 * 128), own, c);
   }
-  return c;
-}
-// C += (transposed tile, 32 columns from 32 db on in the order perm32) x (16 streamed rows from row16 on), p: the lane's 8 of them
+  __device__ __forceinline__ f32x16 cols(unsigned tile, int row16, int db, bf16x8 p, f32x16 c) const {
+    return mfma32(lds_frag_tr_at(tile + col[db & 1][0], tile + col[db & 1][1], (db >> 1) * ROWS * 128 + row16 * 128), p, c);
+  }
+};
 template <int ND, int ROWS>
-__device__ __forceinline__ f32x16 mma_cols(const bf16_t*, const char* tile, int row16, int db, bf16x8 p, f32x16 c, int lane) {
-  return mfma32(lds_frag_tr_sw_perm((const bf16_t*)(tile + (db >> 1) * ROWS * 128), row16, 32 * (db & 1), lane), p, c);
-}
-template <int ND, int ROWS>
-__device__ __forceinline__ f32x16 mma_cols(const float*, const char* tile, int row16, int db, const F8& p, f32x16 c, int lane) {
-  const int col = 32 * db + perm32(lane & 31), row0 = row16 + 8 * (lane >> 5);
+struct LaneAt<float, ND, ROWS> {
+  unsigned row[4], col[8];
+  __device__ __forceinline__ LaneAt(int lane) {
+    const int r = perm32(lane & 31), h = lane >> 5;
 #pragma unroll
-  for (int j = 0; j < 8; ++j)
-    c = mfma_f32(*(const float*)(tile + Tile<float, ND, ROWS>::unit_at(row0 + j, col >> 2) + 4 * (col & 3)), p.v[j], c);
-  return c;
-}
+    for (int i = 0; i < 4; ++i) row[i] = r * ND * 128 + (((2 * i + h) ^ (r & 7)) << 4);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) col[j] = (8 * h + j) * ND * 128 + (((r >> 2) ^ j) << 4) + 4 * (r & 3);
+  }
+  __device__ __forceinline__ f32x16 rows(unsigned tile, int row32, int s, const F8& own, f32x16 c, int left) const {   // left: elements from this step on
+    const int off = (s >> 1) * 128 + row32 * ND * 128;
+    const f32x4 u = lds_load<f32x4>(tile + row[2 * (s & 1)], off);
+    c = mfma_f32(u[0], own.v[0], c);
+    c = mfma_f32(u[1], own.v[1], c);
+    c = mfma_f32(u[2], own.v[2], c);
+    c = mfma_f32(u[3], own.v[3], c);
+    if (left > 8) {
+      const f32x4 w = lds_load<f32x4>(tile + row[2 * (s & 1) + 1], off);
+      c = mfma_f32(w[0], own.v[4], c);
+      c = mfma_f32(w[1], own.v[5], c);
+      c = mfma_f32(w[2], own.v[6], c);
+      c = mfma_f32(w[3], own.v[7], c);
+    }
+    return c;
+  }
+  __device__ __forceinline__ f32x16 cols(unsigned tile, int row16, int db, const F8& p, f32x16 c) const {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c = mfma_f32(lds_load<float>(tile + col[j], db * 128 + row16 * ND * 128), p.v[j], c);
+    return c;
+  }
+};
 __device__ __forceinline__ bf16x8 pack_p(const bf16_t*, const float* p) { return pack8(p); }   // the one rounding of probabilities and dS
 __device__ __forceinline__ F8 pack_p(const float*, const float* p) {
   F8 f;
@@ -215,28 +247,30 @@ __device__ __forceinline__ T* head_of(const im_view_t& v, long b, long row, long
 }
 
 // ---- scores ----
-// hyperbolic tangent to fp32 accuracy: Taylor series to x^11 below 0.35 (next term 1.3e-8 x), above (1 - e) / (1 + e), e = exp(-2 |x|)
-__device__ __forceinline__ float tanh_f32(float x) {
-  const float ax = fabsf(x), u = x * x;
-  const float e = fast_exp2(-2.f * LOG2E * ax);
-  const float big = __builtin_copysignf((1.f - e) * __builtin_amdgcn_rcpf(1.f + e), x);
-  const float small = x + x * u * (-1.f / 3 + u * (2.f / 15 + u * (-17.f / 315 + u * (62.f / 2835 + u * (-1382.f / 155925)))));
-  return ax < 0.35f ? small : big;
+// Hyperbolic tangent of N arguments to fp32 accuracy.  Below 1/2 it is x (1 + u Q(u)), u = x^2, with Q of degree 3 fitted to the
+// smallest relative error there (1.5e-8): 7 multiply-adds, where (1 - e) / (1 + e), e = exp(-2 |x|), takes an exponential and
+// a reciprocal.  Scores rarely come near half of their cap, so the wave looks at its largest argument first (`large`) and
+// takes the exponential only if it has to; an argument gives the same bits either way.
+__device__ __forceinline__ float tanh_small(float x) {
+  const float u = x * x;
+  const float w = __builtin_fmaf(u, __builtin_fmaf(u, __builtin_fmaf(u, __builtin_fmaf(u, 0.01724148f, -0.05304549f), 0.13325879f), -0.33333144f), 1.f);
+  return x * w;
 }
-// Raw product -> score in units of log2.  With a cap *g is what the derivative needs: bf16 g = r (1 - r) = (1 - tanh^2) / 4
-// with r = 1 / (1 + exp(2 x)), tanh x = 1 - 2 r (absolute error 1e-7 of the cap, far below a probability's rounding
-// to bf16); fp32 g = 1 - tanh^2.
-template <class T, bool CAP, bool GRAD>
-__device__ __forceinline__ float score(const CoreArgs& a, float raw, float* g) {
-  if constexpr (!CAP) return raw * a.c_in;
-  else if constexpr (sizeof(T) == 2) {
-    const float r = __builtin_amdgcn_rcpf(1.f + fast_exp2(raw * a.c_in));
-    if constexpr (GRAD) *g = r - r * r;
-    return a.cap2 - 2.f * a.cap2 * r;
+template <int N>
+__device__ __forceinline__ void tanh_of(float (&x)[N], bool large) {
+  if (large) {
+#pragma unroll
+    for (int r = 0; r < N; ++r) {
+      const float ax = fabsf(x[r]), e = fast_exp2(-2.f * LOG2E * ax);
+      const float big = __builtin_copysignf((1.f - e) * __builtin_amdgcn_rcpf(1.f + e), x[r]);
+      float small = tanh_small(x[r]);
+      asm("" : "+v"(small));   // both are computed: a choice, no branch per score
+      x[r] = ax >= 0.5f ? big : small;
+      if ((r & 3) == 3) __builtin_amdgcn_sched_barrier(0);   // few at a time: registers are what limits the waves in flight
+    }
   } else {
-    const float t = tanh_f32(raw * a.c_in);
-    if constexpr (GRAD) *g = 1.f - t * t;
-    return a.cap2 * t;
+#pragma unroll
+    for (int r = 0; r < N; ++r) x[r] = tanh_small(x[r]);
   }
 }
 
@@ -315,15 +349,15 @@ template <class T, int ND, bool FEW> struct CoreCfg {
   static constexpr int ROWS = FEW || sizeof(T) == 4 ? 32 : 64;      // streamed rows of a tile
   static constexpr int TEAM = FEW ? 64 : 64 * CORE_WAVES;           // threads that load a tile together
   static constexpr int OWN = FEW ? 32 : 32 * CORE_WAVES;            // owned rows of a workgroup
-  static constexpr int BUFS = FEW ? 1 : 2;                          // a wave on its own needs no second buffer
-  static constexpr int N = ROWS * Tile<T, ND, ROWS>::CPR / TEAM;    // 16-byte units a thread and tensor
+  static constexpr int BUFS = FEW && sizeof(T) == 4 && ND == 4 ? 1 : 2;   // four teams' pairs of the widest fp32 tiles do not fit the LDS twice
+  static constexpr int N = Tile<T, ND, ROWS>::SLOTS / TEAM;         // 16-byte units a thread and tensor
 };
 
 // LDS of one team
 template <class T, int ND, bool FEW, CoreKernel WHICH>
 struct TeamLds {
   using C = CoreCfg<T, ND, FEW>;
-  char a[C::BUFS][Tile<T, ND, C::ROWS>::BYTES], b[C::BUFS][Tile<T, ND, C::ROWS>::BYTES];   // K, V or Q, dO
+  char tile[C::BUFS][2][Tile<T, ND, C::ROWS>::BYTES];   // K, V or Q, dO
   RowMeta<C::ROWS> meta[C::BUFS];
   typename std::conditional<WHICH == CORE_DKV, QueryMeta<C::ROWS>, char>::type qmeta[C::BUFS];
 };
@@ -331,7 +365,7 @@ template <class T, int ND, bool FEW, CoreKernel WHICH>
 struct CoreLds {
   static constexpr int TEAMS = FEW ? CORE_WAVES : 1;
   __align__(16) TeamLds<T, ND, FEW, WHICH> team[TEAMS];
-  int2 list[CORE_LIST];       // first row; rows | class << 16
+  int4 list[CORE_LIST];       // first row, rows, class, head of the group (dK/dV)
   Range own[CORE_WAVES];
 };
 
@@ -368,33 +402,32 @@ __device__ __forceinline__ Place place_of(const CoreArgs& a, int nord) {
   int k = 0;
   while (k + 1 < nord && (int)tile >= a.tile_prefix[k + 1]) ++k;
   Place p;
-  p.b = (int)b; p.kvh = (int)kvh; p.split = (int)split; p.seg = a.order[k];
+  p.b = __builtin_amdgcn_readfirstlane((int)b);
+  p.kvh = __builtin_amdgcn_readfirstlane((int)kvh);
+  p.split = __builtin_amdgcn_readfirstlane((int)split);
+  k = __builtin_amdgcn_readfirstlane(k);
+  p.seg = a.order[k];
   p.own_n = OWN_KEYS ? a.k_off[p.seg + 1] - a.k_off[p.seg] : (a.q_off[p.seg + 1] - a.q_off[p.seg]) * a.G;
   // the last tile of a segment first: under causality it sees most
-  p.own0 = (a.tile_prefix[k + 1] - 1 - (int)tile) * OWN;
+  p.own0 = (a.tile_prefix[k + 1] - 1 - __builtin_amdgcn_readfirstlane((int)tile)) * OWN;
   return p;
 }
 
-// Streamed tensors as rows; G > 1: row i is position i / G, head i % G of the group
-struct Streamed { const char *a, *b; long a_row, a_head, b_row, b_head; };
-template <class T>
-__device__ __forceinline__ const T* streamed_row(const char* base, long row, long head, int G, int i) {
-  if (G == 1) return (const T*)base + i * row;
-  unsigned t, g;
-  udivmod((unsigned)i, (unsigned)G, t, g);
-  return (const T*)base + t * row + g * head;
-}
-
 // ---- the kernel ----
+// Waves a SIMD: two where the registers of both fit (256 each), one for the widest accumulators.
+template <class T, int ND, CoreKernel WHICH>
+constexpr int core_waves() { return ND == 4 && (sizeof(T) == 4 || WHICH == CORE_DKV) ? 1 : 2; }
+
 template <class T, int ND, bool FEW, bool CAP, bool BIAS, CoreKernel WHICH>
-__global__ __launch_bounds__(64 * CORE_WAVES, 1) void core_kernel(CoreArgs a) {
+__global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, ND, WHICH>())) void core_kernel(CoreArgs a) {
   using C = CoreCfg<T, ND, FEW>;
   using Frag = typename CoreT<T>::Frag;
-  constexpr int ROWS = C::ROWS, EPC = CoreT<T>::EPC, CPR = Tile<T, ND, ROWS>::CPR, BUFS = C::BUFS;
+  using TL = Tile<T, ND, C::ROWS>;
+  constexpr int ROWS = C::ROWS, EPC = CoreT<T>::EPC, BUFS = C::BUFS;
   constexpr bool OWN_KEYS = WHICH == CORE_DKV, BWD = WHICH != CORE_FWD;
   extern __shared__ __align__(16) char lds_raw[];
   auto& lds = *(CoreLds<T, ND, FEW, WHICH>*)lds_raw;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), h = lane >> 5;
   const int tt = FEW ? lane : (int)threadIdx.x;     // thread of the team
   auto& team = lds.team[FEW ? wave : 0];
   const Place at = place_of<OWN_KEYS, C::OWN>(a, a.n_seg);
@@ -440,6 +473,9 @@ __global__ __launch_bounds__(64 * CORE_WAVES, 1) void core_kernel(CoreArgs a) {
       for (int r2 = tt; r2 < ROWS; r2 += C::TEAM) team.meta[i].bad[r2] = 0;
       if (tt == 0) team.meta[i].any_bad = 0;
     }
+    // columns behind the head's end are never written by the copies
+    if (dh < 32 * ND)
+      for (int i = tt; i < BUFS * 2 * TL::SLOTS; i += C::TEAM) ((u32x4*)team.tile)[i] = u32x4{0u, 0u, 0u, 0u};
   }
   __syncthreads();
   Range mine = lds.own[0];
@@ -454,28 +490,22 @@ __global__ __launch_bounds__(64 * CORE_WAVES, 1) void core_kernel(CoreArgs a) {
   }
 
   // ---- the streamed side ----
-  Streamed s;
-  if constexpr (OWN_KEYS) {
-    s.a = (const char*)head_of<const T>(a.q, b, 0, (long)at.kvh * a.G);
-    s.b = (const char*)head_of<const T>(a.d_o, b, 0, (long)at.kvh * a.G);
-    s.a_row = a.q.row; s.a_head = a.q.head; s.b_row = a.d_o.row; s.b_head = a.d_o.head;
-  } else {
-    s.a = (const char*)head_of<const T>(a.k, b, 0, at.kvh);
-    s.b = (const char*)head_of<const T>(a.v, b, 0, at.kvh);
-    s.a_row = a.k.row; s.a_head = 0; s.b_row = a.v.row; s.b_head = 0;
-  }
-  const int G = OWN_KEYS ? a.G : 1;
+  // its rows: keys, or the positions of one query head after another
+  const im_view_t& va = OWN_KEYS ? a.q : a.k;
+  const im_view_t& vb = OWN_KEYS ? a.d_o : a.v;
+  const int head0 = OWN_KEYS ? at.kvh * a.G : at.kvh;
+  const T *base_a = head_of<const T>(va, b, 0, head0), *base_b = head_of<const T>(vb, b, 0, head0);
   const bool vec_a = a.vec & (OWN_KEYS ? VEC_Q : VEC_K), vec_b = a.vec & (OWN_KEYS ? VEC_DO : VEC_V);
   const unsigned live = OWN_KEYS ? a.k_live[at.seg] : a.q_live[at.seg];
   const bool scan = a.causal || a.q_doc || (a.key_pad && !OWN_KEYS);   // classes that depend on the streamed rows' data
   auto stream_len = [&](int j) {   // rows of streamed segment j that count
-    if (OWN_KEYS) return (a.q_off[j + 1] - a.q_off[j]) * a.G;
+    if (OWN_KEYS) return a.q_off[j + 1] - a.q_off[j];
     const int n = a.k_off[j + 1] - a.k_off[j];
     return a.valid_len ? min(n, max(a.valid_len[b * a.n_seg + j], 0)) : n;
   };
   int total = 0;
   for (int j = 0; j < a.n_seg; ++j)
-    if ((live >> j) & 1u) total += (stream_len(j) + ROWS - 1) / ROWS;
+    if ((live >> j) & 1u) total += (stream_len(j) + ROWS - 1) / ROWS * (OWN_KEYS ? a.G : 1);
   if (!mine.any) total = 0;
   const int first = (int)((long)total * at.split / a.splits), last = (int)((long)total * (at.split + 1) / a.splits);
 
@@ -486,65 +516,66 @@ __global__ __launch_bounds__(64 * CORE_WAVES, 1) void core_kernel(CoreArgs a) {
     acc1[d] = zero16();
     if constexpr (WHICH == CORE_DKV) acc2[d] = zero16();
   }
-  float m = -3.402823466e38f, l = 0.f;
+  constexpr float LOWEST = -3.402823466e38f;
+  float m = 0.f, l = 0.f, most = LOWEST;   // reference, sum, and by how much a score may exceed the reference
   // A slope's gradient is -sum dS gap.  delta stems from a forward that rounded its probabilities; by how much it is off is what
   // is left of the row's sum of dS (exactly 0 otherwise), and that part is taken back:  -sum (dS - rest P) gap.
   float dslope = 0.f, rest = 0.f, mean_gap = 0.f;
 
-  u32x4 ra[C::N], rb[C::N];
+  // Streamed rows go from global memory into LDS by asynchronous copies, one tile ahead, without staging registers.  A thread's
+  // unit i of a tile: byte offset off_a / off_b from the tile's first row.
+  unsigned off_a[C::N], off_b[C::N];
+  bool has[C::N];
+#pragma unroll
+  for (int i = 0; i < C::N; ++i) {
+    const int u = tt + i * C::TEAM, row = TL::row_of(u), c = TL::unit_of(u);
+    off_a[i] = (unsigned)(row * va.row * (long)sizeof(T)) + 16 * c;
+    off_b[i] = (unsigned)(row * vb.row * (long)sizeof(T)) + 16 * c;
+    has[i] = c * EPC < dh;
+  }
   RowInfo ri = {0.f, 0.f, 0};
   float r_lse2 = 0.f, r_delta = 0.f, r_slope2 = 0.f;
   int stamp = 0;
-
-  // global -> registers of one list entry
-  auto fetch = [&](int2 e) {
-    const int row0 = e.x, n = e.y & 0xffff;
+  // one tensor's tile; rows behind the n-th repeat the last one (no pair of theirs counts)
+  auto copy = [&](const T* from, const im_view_t& view, const unsigned (&off)[C::N], bool vec, char* to, int n) {
+    if (vec) {
 #pragma unroll
-    for (int i = 0; i < C::N; ++i) {
-      const int u = tt + i * C::TEAM, row = u / CPR, c = u % CPR;
-      u32x4 z = {0u, 0u, 0u, 0u};
-      ra[i] = rb[i] = z;
-      if (row < n) {
-        ra[i] = load_unit(streamed_row<T>(s.a, s.a_row, s.a_head, G, row0 + row), c * EPC, dh, vec_a);
-        rb[i] = load_unit(streamed_row<T>(s.b, s.b_row, s.b_head, G, row0 + row), c * EPC, dh, vec_b);
+      for (int i = 0; i < C::N; ++i) {
+        unsigned o = off[i];
+        if (n < ROWS) {
+          const int u = tt + i * C::TEAM;
+          o = (unsigned)(min(TL::row_of(u), n - 1) * view.row * (long)sizeof(T)) + 16 * TL::unit_of(u);
+        }
+        if (has[i]) dma16_off(from, o, to + (i * C::TEAM + (FEW ? 0 : wave * 64)) * 16);
+      }
+    } else {   // element by element, through registers
+#pragma unroll 1
+      for (int i = 0; i < C::N; ++i) {
+        const int u = tt + i * C::TEAM;
+        *(u32x4*)(to + u * 16) = load_unit(from + min(TL::row_of(u), n - 1) * view.row, TL::unit_of(u) * EPC, dh, false);
       }
     }
+  };
+  auto fetch = [&](int4 e, int buf) {
+    const int row0 = __builtin_amdgcn_readfirstlane(e.x), n = __builtin_amdgcn_readfirstlane(e.y);
+    const int g = OWN_KEYS ? __builtin_amdgcn_readfirstlane(e.w) : 0;
+    copy(base_a + row0 * va.row + g * va.head, va, off_a, vec_a, team.tile[buf][0], n);
+    copy(base_b + row0 * vb.row + g * vb.head, vb, off_b, vec_b, team.tile[buf][1], n);
     if (tt < ROWS) {
       const bool ok = tt < n;
       if constexpr (OWN_KEYS) {
-        unsigned t = (unsigned)(row0 + tt), g = 0;
-        if (a.G > 1) udivmod(t, (unsigned)a.G, t, g);
-        ri = query_info(a, b, (int)t, ok);
-        const int head = at.kvh * a.G + (int)g;
-        const long st = ((long)b * a.H + head) * a.Tq + (int)t;
+        ri = query_info(a, b, row0 + tt, ok);
+        const int head = head0 + g;
+        const long st = ((long)b * a.H + head) * a.Tq + row0 + tt;
         r_lse2 = ok ? a.lse2[st] : __builtin_inff();
         r_delta = ok ? a.delta[st] : 0.f;
         r_slope2 = BIAS && ok ? a.slope[head] * LOG2E : 0.f;
       } else ri = key_info(a, b, row0 + tt, ok);
     }
   };
-  // registers -> LDS
-  auto put = [&](int buf, int cls) {
-    char *ta = team.a[buf], *tb = team.b[buf];
-#pragma unroll
-    for (int i = 0; i < C::N; ++i) {
-      const int u = tt + i * C::TEAM, row = u / CPR, c = u % CPR;
-      u32x4 x = ra[i], y = rb[i];
-      if (cls == TILE_PART) {
-        bool odd = false;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) odd |= odd_bits(T(), x[w]) | odd_bits(T(), y[w]);
-        if (odd) {
-#pragma unroll
-          for (int w = 0; w < 4; ++w) { x[w] = clean_bits(T(), x[w]); y[w] = clean_bits(T(), y[w]); }
-          team.meta[buf].bad[row] = stamp;
-          team.meta[buf].any_bad = stamp;
-        }
-      }
-      const int to = Tile<T, ND, ROWS>::unit_at(row, c);
-      *(u32x4*)(ta + to) = x;
-      *(u32x4*)(tb + to) = y;
-    }
+  // the copies of a tile are complete, for this wave; its rows' numbers go to LDS
+  auto arrive = [&](int buf) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     if (tt < ROWS) {
       team.meta[buf].order[tt] = ri.order;
       team.meta[buf].pos[tt] = ri.pos;
@@ -556,152 +587,209 @@ __global__ __launch_bounds__(64 * CORE_WAVES, 1) void core_kernel(CoreArgs a) {
       }
     }
   };
+  // values of a tile with masked pairs that are not finite: 0 in their place, and a mark on their row
+  auto clean = [&](int buf) {
+    u32x4* units = (u32x4*)team.tile[buf];
+#pragma unroll
+    for (int i = 0; i < 2 * C::N; ++i) {
+      const int u = tt + i * C::TEAM;
+      if (TL::unit_of(u % TL::SLOTS) * EPC >= 32 * ND) continue;   // half a panel that nothing reads or writes (ND = 1)
+      u32x4 x = units[u];
+      bool odd = false;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) odd |= odd_bits(T(), x[w]);
+      if (odd) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) x[w] = clean_bits(T(), x[w]);
+        units[u] = x;
+        team.meta[buf].bad[TL::row_of(u % TL::SLOTS)] = stamp;
+        team.meta[buf].any_bad = stamp;
+      }
+    }
+  };
 
-  // one block of 32 streamed rows
+  // one block of 32 streamed rows; part: with masked pairs
+  const LaneAt<T, ND, ROWS> at_lane(lane);
   auto block = [&](int buf, int row32, bool part) {
-    const char *ta = team.a[buf], *tb = team.b[buf];
+    const unsigned ta = lds_at(team.tile[buf][0]), tb = lds_at(team.tile[buf][1]);
     const RowMeta<ROWS>& meta = team.meta[buf];
     f32x16 sc = zero16(), dp;
 #pragma unroll
     for (int st = 0; st < 2 * ND; ++st)
-      if (sizeof(T) == 2 || 16 * st < dh) sc = mma_rows(row_frag<ND, ROWS>((const T*)nullptr, ta, row32, st, lane), own1[st], sc, dh - 16 * st);
+      if (sizeof(T) == 2 || 16 * st < dh) sc = at_lane.rows(ta, row32, st, own1[st], sc, dh - 16 * st);
     if constexpr (BWD) {
       dp = zero16();
 #pragma unroll
       for (int st = 0; st < 2 * ND; ++st)
-        if (sizeof(T) == 2 || 16 * st < dh) dp = mma_rows(row_frag<ND, ROWS>((const T*)nullptr, tb, row32, st, lane), own2[st], dp, dh - 16 * st);
+        if (sizeof(T) == 2 || 16 * st < dh) dp = at_lane.rows(tb, row32, st, own2[st], dp, dh - 16 * st);
     }
-    float x[16], g[16];
+    const float k = CAP ? a.cap2 : a.c_in;   // raw score, or tangent, -> score in units of log2
+    bool large = false;
+    if constexpr (CAP) {
+      float top = fabsf(sc[0]);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) x[r] = score<T, CAP, BWD>(a, sc[r], &g[r]);
-    // register r: streamed row row32 + 16 (r / 8) + 8 h + r % 8
-    float gap[BIAS ? 16 : 1];
-    if constexpr (BIAS) {
+      for (int r = 1; r < 16; ++r) top = fmaxf(top, fabsf(sc[r]));
+      large = __any(top * a.c_in >= 0.5f);
+    }
+    // Eight rows at a time: register 8 i + e of a product is streamed row row0 + e.  x: score less the reference (forward) or the row's
+    // log-sum-exp (backward), -inf where the pair is masked; g: derivative of the cap; gap: distance.
+    auto scores = [&](int i, float (&x)[8], float (&g)[CAP && BWD ? 8 : 1], float (&gap)[BIAS ? 8 : 1]) {
+      const int row0 = row32 + 16 * i + 8 * h;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int row = row32 + 16 * (r >> 3) + 8 * h + (r & 7);
-        gap[r] = fabsf(meta.pos[row] - own.pos);
-        float sl = own_slope2;
-        if constexpr (OWN_KEYS) sl = team.qmeta[buf].slope2[row];
-        x[r] -= sl * gap[r];
+      for (int e = 0; e < 8; ++e) x[e] = CAP ? sc[8 * i + e] * a.c_in : sc[8 * i + e];
+      if constexpr (CAP) tanh_of(x, large);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if constexpr (CAP && BWD) g[e] = __builtin_fmaf(-x[e], x[e], 1.f);
+        float ref = m;
+        if constexpr (WHICH == CORE_DQ) ref = own_lse2;
+        if constexpr (WHICH == CORE_DKV) ref = team.qmeta[buf].lse2[row0 + e];
+        x[e] = __builtin_fmaf(x[e], k, -ref);
+        if constexpr (BIAS) {
+          float sl = own_slope2;
+          if constexpr (OWN_KEYS) sl = team.qmeta[buf].slope2[row0 + e];
+          gap[e] = fabsf(meta.pos[row0 + e] - own.pos);
+          x[e] = __builtin_fmaf(-sl, gap[e], x[e]);
+        }
       }
-    }
-    if (part) {
-      const bool bad = meta.any_bad == stamp;
+      if (part) {
+        const bool bad = meta.any_bad == stamp;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int row = row32 + 16 * (r >> 3) + 8 * h + (r & 7);
-        const float o = meta.order[row];
-        const bool sees = (OWN_KEYS ? own.order <= o : o <= own.order) && meta.doc[row] == own.doc;
-        if (bad && meta.bad[row] == stamp) x[r] = __builtin_nanf("");
-        x[r] = sees ? x[r] : IM_NEG_INF;
+        for (int e = 0; e < 8; ++e) {
+          const float o = meta.order[row0 + e];
+          const bool sees = (OWN_KEYS ? own.order <= o : o <= own.order) && meta.doc[row0 + e] == own.doc;
+          if (bad && meta.bad[row0 + e] == stamp) x[e] = __builtin_nanf("");
+          x[e] = sees ? x[e] : IM_NEG_INF;
+        }
       }
-    }
+    };
+    Frag p[2], q[2];
     if constexpr (WHICH == CORE_FWD) {
-      float mx = x[0];
+      float x[2][8], none[1], gap[BIAS ? 8 : 1];
+      float mx = IM_NEG_INF;
 #pragma unroll
-      for (int r = 1; r < 16; ++r) mx = fmaxf(mx, x[r]);
-      mx = fmaxf(mx, other_half(mx));
-      // a row's reference moves only when a score exceeds it by 8: probabilities stay below 2^8, and no row's bits depend on another's
-      if (__any(mx > m + 8.f)) {
-        const float to = mx > m + 8.f ? mx : m, f = fast_exp2(m - to);
-        m = to;
+      for (int i = 0; i < 2; ++i) {
+        scores(i, x[i], none, gap);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) mx = fmaxf(mx, x[i][e]);
+      }
+      // A row's reference is its first block's largest score and moves only when a score exceeds it by 8: probabilities stay below
+      // 2^8, and no row's bits depend on another's.
+      if (__any(mx > most)) {
+        mx = fmaxf(mx, other_half(mx));
+        const float by = mx > most ? mx : 0.f;
+        const float f = by > 0.f ? fast_exp2(-by) : 1.f;   // (a first reference below 0 has nothing to scale yet)
+        if (mx > most) most = 8.f;
+        m += by;
         l *= f;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[i][e] -= by;
 #pragma unroll
         for (int d = 0; d < ND; ++d)
 #pragma unroll
           for (int r = 0; r < 16; ++r) acc1[d][r] *= f;
       }
 #pragma unroll
-      for (int r = 0; r < 16; ++r) { x[r] = fast_exp2(x[r] - m); l += x[r]; }
+      for (int i = 0; i < 2; ++i) {
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const Frag p = pack_p((const T*)nullptr, x + 8 * k);
-#pragma unroll
-        for (int d = 0; d < ND; ++d)
-          if (sizeof(T) == 2 || 32 * d < dh) acc1[d] = mma_cols<ND, ROWS>((const T*)nullptr, tb, row32 + 16 * k, d, p, acc1[d], lane);
+        for (int e = 0; e < 8; ++e) { x[i][e] = fast_exp2(x[i][e]); l += x[i][e]; }
+        p[i] = pack_p((const T*)nullptr, x[i]);
       }
     } else {
-      float ds[16];
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int row = row32 + 16 * (r >> 3) + 8 * h + (r & 7);
-        float lse2 = own_lse2, delta = own_delta;
-        if constexpr (OWN_KEYS) { lse2 = team.qmeta[buf].lse2[row]; delta = team.qmeta[buf].delta[row]; }
-        // a masked score is -inf, also where the row sees nothing at all (lse2 = -inf)
-        x[r] = part && x[r] == IM_NEG_INF ? 0.f : fast_exp2(x[r] - lse2);
-        ds[r] = x[r] * (dp[r] - delta);
-        const bool none = part && x[r] == 0.f;   // the other product of a masked pair, and its score, may be anything
-        if (none) ds[r] = 0.f;
-        if constexpr (BIAS && WHICH == CORE_DQ) {
-          dslope -= ds[r] * gap[r];
-          rest += ds[r];
-          mean_gap += x[r] * gap[r];
+      for (int i = 0; i < 2; ++i) {
+        const int row0 = row32 + 16 * i + 8 * h;
+        float x[8], ds[8], g[CAP ? 8 : 1], gap[BIAS ? 8 : 1];
+        scores(i, x, g, gap);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          float delta = own_delta;
+          if constexpr (OWN_KEYS) delta = team.qmeta[buf].delta[row0 + e];
+          x[e] = fast_exp2(x[e]);
+          ds[e] = x[e] * (dp[8 * i + e] - delta);
+          if constexpr (BIAS && WHICH == CORE_DQ) {
+            dslope -= ds[e] * gap[e];
+            rest += ds[e];
+            mean_gap += x[e] * gap[e];
+          }
+          if constexpr (CAP) ds[e] *= g[e];
         }
-        if constexpr (CAP) ds[r] = none ? 0.f : ds[r] * g[r];
-      }
+        // A masked pair has x = 0.  Its other factors are finite where keys are streamed (or the owned row's results are lost anyway); an owned
+        // key that nobody sees, and the statistics of a query that does not see it, may be anything.
+        if (OWN_KEYS && part) {
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const Frag q = pack_p((const T*)nullptr, ds + 8 * k);
-#pragma unroll
-        for (int d = 0; d < ND; ++d)
-          if (sizeof(T) == 2 || 32 * d < dh) acc1[d] = mma_cols<ND, ROWS>((const T*)nullptr, ta, row32 + 16 * k, d, q, acc1[d], lane);
-        if constexpr (WHICH == CORE_DKV) {
-          const Frag p = pack_p((const T*)nullptr, x + 8 * k);
-#pragma unroll
-          for (int d = 0; d < ND; ++d)
-            if (sizeof(T) == 2 || 32 * d < dh) acc2[d] = mma_cols<ND, ROWS>((const T*)nullptr, tb, row32 + 16 * k, d, p, acc2[d], lane);
+          for (int e = 0; e < 8; ++e) ds[e] = x[e] == 0.f ? 0.f : ds[e];
         }
+        if constexpr (WHICH == CORE_DKV) p[i] = pack_p((const T*)nullptr, x);
+        q[i] = pack_p((const T*)nullptr, ds);
       }
     }
+    // 32 columns of the second products; WHICH == CORE_DKV: both
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int d = 0; d < ND; ++d)
+        if (sizeof(T) == 2 || 32 * d < dh) {
+          if constexpr (WHICH == CORE_FWD) acc1[d] = at_lane.cols(tb, row32 + 16 * i, d, p[i], acc1[d]);
+          else acc1[d] = at_lane.cols(ta, row32 + 16 * i, d, q[i], acc1[d]);
+          if constexpr (WHICH == CORE_DKV) acc2[d] = at_lane.cols(tb, row32 + 16 * i, d, p[i], acc2[d]);
+        }
   };
 
   for (int lo = first; lo < last; lo += CORE_LIST) {
     const int n = min(CORE_LIST, last - lo);
     // ---- list of the next tiles ----
     if ((int)threadIdx.x < n) {
-      int t = lo + (int)threadIdx.x, j = 0, len = 0;
+      int t = lo + (int)threadIdx.x, j = 0, len = 0, g = 0;
       for (; j < a.n_seg; ++j) {
         if (!((live >> j) & 1u)) continue;
         len = stream_len(j);
-        const int nt = (len + ROWS - 1) / ROWS;
-        if (t < nt) break;
-        t -= nt;
+        const int nt = (len + ROWS - 1) / ROWS, all = OWN_KEYS ? nt * a.G : nt;
+        if (t < all) {
+          if (OWN_KEYS && a.G > 1) { g = t / nt; t -= g * nt; }
+          break;
+        }
+        t -= all;
       }
-      const int row0 = (OWN_KEYS ? a.q_off[j] * a.G : a.k_off[j]) + t * ROWS, rows = min(ROWS, len - t * ROWS);
+      const int row0 = (OWN_KEYS ? a.q_off[j] : a.k_off[j]) + t * ROWS, rows = min(ROWS, len - t * ROWS);
       const bool full = rows == ROWS && mine.all && !scan;
-      lds.list[threadIdx.x] = make_int2(row0, rows | (full ? TILE_FULL : TILE_PART) << 16);
+      lds.list[threadIdx.x] = make_int4(row0, rows, full ? TILE_FULL : TILE_PART, g);
     }
     __syncthreads();
     if (scan) {
       for (int i = wave; i < n; i += CORE_WAVES) {
-        const int2 e = lds.list[i];
-        const int rows = e.y & 0xffff;
-        const bool in = lane < rows;
-        unsigned t = (unsigned)(e.x + lane), g = 0;
-        if (OWN_KEYS && a.G > 1) udivmod(t, (unsigned)a.G, t, g);
-        const RowInfo info = OWN_KEYS ? query_info(a, b, (int)t, in) : key_info(a, b, (int)t, in);
+        const int4 e = lds.list[i];
+        const bool in = lane < e.y;
+        const RowInfo info = OWN_KEYS ? query_info(a, b, e.x + lane, in) : key_info(a, b, e.x + lane, in);
         const Range r = range_of(info, in);
-        const int cls = OWN_KEYS ? tile_class(mine, r, rows == ROWS) : tile_class(r, mine, rows == ROWS);
-        if (lane == 0) lds.list[i].y = rows | cls << 16;
+        const int cls = OWN_KEYS ? tile_class(mine, r, e.y == ROWS) : tile_class(r, mine, e.y == ROWS);
+        if (lane == 0) lds.list[i].z = cls;
       }
       __syncthreads();
     }
     // ---- walk over it ----
     const int step = FEW ? CORE_WAVES : 1;
     auto next = [&](int i) {
-      while (i < n && (lds.list[i].y >> 16) == TILE_SKIP) i += step;
+      while (i < n && lds.list[i].z == TILE_SKIP) i += step;
       return i;
     };
     int i = next(FEW ? wave : 0), buf = 0;
-    if (i < n) fetch(lds.list[i]);
+    if (BUFS == 2 && i < n) fetch(lds.list[i], 0);
     while (i < n) {
-      const int cls = __builtin_amdgcn_readfirstlane(lds.list[i].y >> 16);
+      const int cls = __builtin_amdgcn_readfirstlane(lds.list[i].z);
+      if (BUFS == 1) fetch(lds.list[i], 0);
+      arrive(buf);
+      team_sync<FEW>();   // all waves' copies are there, and nobody reads the other buffer any more
       ++stamp;
-      put(buf, cls);
-      team_sync<FEW>();
       i = next(i + step);
-      if (i < n) fetch(lds.list[i]);
+      if (BUFS == 2 && i < n) fetch(lds.list[i], buf ^ 1);
+      if (cls == TILE_PART) {
+        clean(buf);
+        team_sync<FEW>();
+      }
+#pragma unroll
       for (int r = 0; r < ROWS; r += 32) block(buf, r, cls == TILE_PART);
       if constexpr (FEW) team_sync<FEW>();
       buf ^= BUFS - 1;
@@ -710,7 +798,10 @@ __global__ __launch_bounds__(64 * CORE_WAVES, 1) void core_kernel(CoreArgs a) {
   }
 
   // ---- results ----
-  if constexpr (WHICH == CORE_FWD) l += other_half(l);
+  if constexpr (WHICH == CORE_FWD) {
+    l += other_half(l);
+    if (most == LOWEST) m = LOWEST;   // nothing seen
+  }
   if constexpr (BIAS && WHICH == CORE_DQ) {
     dslope += other_half(dslope);
     rest += other_half(rest);
@@ -773,7 +864,7 @@ __global__ __launch_bounds__(64 * CORE_WAVES, 1) void core_kernel(CoreArgs a) {
       if (h == 0) { a.part_ml[2 * row] = m; a.part_ml[2 * row + 1] = l; }
       return;
     }
-    const float inv = l == 0.f ? 0.f : 1.f / l, lse2 = m + log2f(l);
+    const float inv = l == 0.f ? 0.f : 1.f / l, lse2 = l == 0.f ? IM_NEG_INF : m + log2f(l);
     store_row<T, ND>(head_of<T>(a.o, b, own_row, own_head), dh, a.vec & VEC_O, h, acc1, inv);
     if (a.o32) store_row<float, ND>(a.o32 + own_stat * dh, dh, dh % 4 == 0, h, acc1, inv);
     if (h == 0) {
@@ -781,10 +872,10 @@ __global__ __launch_bounds__(64 * CORE_WAVES, 1) void core_kernel(CoreArgs a) {
       if (a.lse2) a.lse2[own_stat] = lse2;
     }
   } else if constexpr (WHICH == CORE_DQ) {
-    store_row<T, ND>(head_of<T>(a.dq, b, own_row, own_head), dh, a.vec & VEC_DQ, h, acc1, a.d_scale);
+    store_row<T, ND>(head_of<T>(a.dq, b, own_row, own_head), dh, a.vec & VEC_DQ, h, acc1, a.scale);
     if (BIAS && a.dslope_rows && h == 0) a.dslope_rows[own_stat] = dslope + rest * mean_gap;
   } else {
-    store_row<T, ND>(head_of<T>(a.dk, b, own_row, own_head), dh, a.vec & VEC_DK, h, acc1, a.d_scale);
+    store_row<T, ND>(head_of<T>(a.dk, b, own_row, own_head), dh, a.vec & VEC_DK, h, acc1, a.scale);
     store_row<T, ND>(head_of<T>(a.dv, b, own_row, own_head), dh, a.vec & VEC_DV, h, acc2, 1.f);
   }
 }
