@@ -15,7 +15,7 @@
 // of the softmax's exponential, each four times as long as an ordinary instruction -- except in fp32 from head
 // dimension 64 on, where the fp32 matrix rate does.
 //
-// Which streamed tiles are visited is decided from the data, once per workgroup and 256 tiles: a tile in which no owned row
+// Which streamed tiles are visited is decided from the data, once per workgroup and 64 tiles: a tile in which no owned row
 // sees any streamed row is skipped, one in which every owned row sees every streamed row takes the path without
 // comparisons.  Both sides carry one number for the order in time: streamed row visible <=> its k_pos <= the owned q_pos
 // (or the other way round for dK/dV), with k_pos = -inf for free keys (no causality, prefix), NaN for padding.
@@ -32,7 +32,7 @@
 namespace imattn {
 
 constexpr int CORE_WAVES = 4;
-constexpr int CORE_LIST = 256;   // streamed tiles classified at a time
+constexpr int CORE_LIST = 64;    // streamed tiles classified at a time
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -150,12 +150,15 @@ __device__ __forceinline__ u32x4 load_unit(const T* head, int at, int dh, bool v
   u32x4 u = {0u, 0u, 0u, 0u};
   if (at >= dh) return u;
   if (vec) return *(const u32x4*)(head + at);
-  if constexpr (sizeof(T) == 2) {
+  constexpr int E = 16 / (int)sizeof(T);
+  T v[E];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) if (at + e < dh) u[e >> 1] |= (unsigned)head[at + e] << (16 * (e & 1));
-  } else {
+  for (int e = 0; e < E; ++e) v[e] = head[min(at + e, dh - 1)];   // no branches: all loads are in flight together
 #pragma unroll
-    for (int e = 0; e < 4; ++e) if (at + e < dh) u[e] = __float_as_uint(head[at + e]);
+  for (int e = 0; e < E; ++e) {
+    const bool is = at + e < dh;
+    if constexpr (sizeof(T) == 2) u[e >> 1] |= (is ? (unsigned)v[e] : 0u) << (16 * (e & 1));
+    else u[e] = is ? __float_as_uint(v[e]) : 0u;
   }
   return u;
 }
@@ -280,38 +283,47 @@ enum { TILE_SKIP = 0, TILE_FULL = 1, TILE_PART = 2 };
 // per streamed row in LDS
 template <int ROWS>
 struct __align__(16) RowMeta {
-  float order[ROWS];   // k_pos (-inf: free, NaN: no key) when keys are streamed, q_pos (+inf: sees all, NaN: no row) when queries are
-  float pos[ROWS];     // position for the bias
+  float pos[ROWS];     // position
   int doc[ROWS];
+  float order[ROWS];   // (first the key's padding byte;) k_pos (-inf: free, NaN: no key) when keys are streamed, q_pos (+inf: sees all, NaN: no row) when queries are
   int bad[ROWS];       // == number of the tile: holds a value that is not finite
   int any_bad;
 };
 template <int ROWS>
 struct __align__(16) QueryMeta {     // dK/dV only
-  float lse2[ROWS], delta[ROWS], slope2[ROWS];
+  float lse2[ROWS], delta[ROWS];
 };
 
 struct RowInfo { float order, pos; int doc; };
+struct RowRaw { float pos; int doc; unsigned pad; };
 
-__device__ __forceinline__ RowInfo key_info(const CoreArgs& a, long b, int row, bool ok) {
-  RowInfo i = {__builtin_nanf(""), 0.f, 0};
-  if (!ok) return i;
-  const long at = b * a.Tk + row;
-  if (a.k_doc) i.doc = a.k_doc[at];
-  if (a.k_pos) i.pos = a.k_pos[at];
-  i.order = a.causal ? i.pos : IM_NEG_INF;
-  if (a.prefix && i.pos < a.prefix[b]) i.order = IM_NEG_INF;
-  if (a.key_pad && a.key_pad[at]) i.order = __builtin_nanf("");
-  return i;
+__device__ __forceinline__ RowRaw key_raw(const CoreArgs& a, long b, int row, bool ok) {
+  RowRaw r = {0.f, 0, 1u};
+  if (ok) {
+    const long at = b * a.Tk + row;
+    r.pad = 0u;
+    if (a.k_doc) r.doc = a.k_doc[at];
+    if (a.k_pos) r.pos = a.k_pos[at];
+    if (a.key_pad) r.pad = a.key_pad[at];
+  }
+  return r;
 }
-__device__ __forceinline__ RowInfo query_info(const CoreArgs& a, long b, int row, bool ok) {
-  RowInfo i = {__builtin_nanf(""), 0.f, 0};
-  if (!ok) return i;
-  const long at = b * a.Tq + row;
-  if (a.q_doc) i.doc = a.q_doc[at];
-  if (a.q_pos) i.pos = a.q_pos[at];
-  i.order = a.causal ? i.pos : __builtin_inff();
-  return i;
+__device__ __forceinline__ RowInfo key_info(const CoreArgs& a, float prefix, const RowRaw& r) {
+  const float order = a.causal && !(r.pos < prefix) ? r.pos : IM_NEG_INF;
+  return {r.pad ? __builtin_nanf("") : order, r.pos, r.doc};
+}
+__device__ __forceinline__ RowRaw query_raw(const CoreArgs& a, long b, int row, bool ok) {
+  RowRaw r = {0.f, 0, 1u};
+  if (ok) {
+    const long at = b * a.Tq + row;
+    r.pad = 0u;
+    if (a.q_doc) r.doc = a.q_doc[at];
+    if (a.q_pos) r.pos = a.q_pos[at];
+  }
+  return r;
+}
+__device__ __forceinline__ RowInfo query_info(const CoreArgs& a, const RowRaw& r) {
+  return {r.pad ? __builtin_nanf("") : a.causal ? r.pos : __builtin_inff(), r.pos, r.doc};
 }
 
 // Smallest and largest order and document of the rows with ok, over the lanes of a wave
@@ -349,7 +361,9 @@ template <class T, int ND, bool FEW> struct CoreCfg {
   static constexpr int ROWS = FEW || sizeof(T) == 4 ? 32 : 64;      // streamed rows of a tile
   static constexpr int TEAM = FEW ? 64 : 64 * CORE_WAVES;           // threads that load a tile together
   static constexpr int OWN = FEW ? 32 : 32 * CORE_WAVES;            // owned rows of a workgroup
-  static constexpr int BUFS = FEW && sizeof(T) == 4 && ND == 4 ? 1 : 2;   // four teams' pairs of the widest fp32 tiles do not fit the LDS twice
+  // Tiles in LDS.  A workgroup's copies run two tiles ahead where the LDS of two workgroups a CU allows, a wave's on its own one ahead; four
+  // teams' pairs of the widest fp32 tiles do not fit the LDS twice.
+  static constexpr int BUFS = FEW && sizeof(T) == 4 && ND == 4 ? 1 : FEW || ND == 4 ? 2 : 3;
   static constexpr int N = Tile<T, ND, ROWS>::SLOTS / TEAM;         // 16-byte units a thread and tensor
 };
 
@@ -442,7 +456,8 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, ND, WHICH>())) void
   const int own_head = OWN_KEYS ? at.kvh : at.kvh * a.G + (int)own_g;
   bool own_valid = in_range;
   if (OWN_KEYS && a.valid_len) own_valid = in_range && (int)own_t < a.valid_len[b * a.n_seg + at.seg];
-  const RowInfo own = OWN_KEYS ? key_info(a, b, own_row, own_valid) : query_info(a, b, own_row, own_valid);
+  const float prefix = a.prefix ? a.prefix[b] : IM_NEG_INF;
+  const RowInfo own = OWN_KEYS ? key_info(a, prefix, key_raw(a, b, own_row, own_valid)) : query_info(a, query_raw(a, b, own_row, own_valid));
   const long own_stat = ((long)b * a.H + own_head) * a.Tq + own_row;   // of a query row
 
   Frag own1[2 * ND], own2[BWD ? 2 * ND : 1];   // Q (and dO), or K and V
@@ -533,8 +548,6 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, ND, WHICH>())) void
     off_b[i] = (unsigned)(row * vb.row * (long)sizeof(T)) + 16 * c;
     has[i] = c * EPC < dh;
   }
-  RowInfo ri = {0.f, 0.f, 0};
-  float r_lse2 = 0.f, r_delta = 0.f, r_slope2 = 0.f;
   int stamp = 0;
   // one tensor's tile; rows behind the n-th repeat the last one (no pair of theirs counts)
   auto copy = [&](const T* from, const im_view_t& view, const unsigned (&off)[C::N], bool vec, char* to, int n) {
@@ -556,35 +569,46 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, ND, WHICH>())) void
       }
     }
   };
+  const bool with_pos = a.causal || BIAS;
+  const int* docs = OWN_KEYS ? a.q_doc : a.k_doc;
+  const float* poss = OWN_KEYS ? a.q_pos : a.k_pos;
+  const int own_side = OWN_KEYS ? a.Tq : a.Tk;   // (rows of the streamed side)
+  const int n_meta = (FEW || wave == 0) ? (with_pos ? 1 : 0) + (docs ? 1 : 0) + (!OWN_KEYS && a.key_pad ? 1 : 0) + (OWN_KEYS ? 2 : 0) : 0;
+  const int copies = (vec_a && vec_b) ? 2 * C::N + n_meta : 0;   // this wave's copies of a tile in flight; 0: they are waited for at once
   auto fetch = [&](int4 e, int buf) {
     const int row0 = __builtin_amdgcn_readfirstlane(e.x), n = __builtin_amdgcn_readfirstlane(e.y);
     const int g = OWN_KEYS ? __builtin_amdgcn_readfirstlane(e.w) : 0;
     copy(base_a + row0 * va.row + g * va.head, va, off_a, vec_a, team.tile[buf][0], n);
     copy(base_b + row0 * vb.row + g * vb.head, vb, off_b, vec_b, team.tile[buf][1], n);
     if (tt < ROWS) {
-      const bool ok = tt < n;
+      const unsigned r = (unsigned)min(tt, n - 1);
+      const long at0 = (long)b * own_side + row0;
+      if (with_pos) dma4_off(poss + at0, 4 * r, team.meta[buf].pos);
+      if (docs) dma4_off(docs + at0, 4 * r, team.meta[buf].doc);
+      if (!OWN_KEYS && a.key_pad) dma1_off(a.key_pad + at0, r, team.meta[buf].order);
       if constexpr (OWN_KEYS) {
-        ri = query_info(a, b, row0 + tt, ok);
-        const int head = head0 + g;
-        const long st = ((long)b * a.H + head) * a.Tq + row0 + tt;
-        r_lse2 = ok ? a.lse2[st] : __builtin_inff();
-        r_delta = ok ? a.delta[st] : 0.f;
-        r_slope2 = BIAS && ok ? a.slope[head] * LOG2E : 0.f;
-      } else ri = key_info(a, b, row0 + tt, ok);
+        const long st = ((long)b * a.H + head0 + g) * a.Tq + row0;
+        dma4_off(a.lse2 + st, 4 * r, team.qmeta[buf].lse2);
+        dma4_off(a.delta + st, 4 * r, team.qmeta[buf].delta);
+      }
     }
   };
-  // the copies of a tile are complete, for this wave; its rows' numbers go to LDS
-  auto arrive = [&](int buf) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    if (tt < ROWS) {
-      team.meta[buf].order[tt] = ri.order;
-      team.meta[buf].pos[tt] = ri.pos;
-      team.meta[buf].doc[tt] = ri.doc;
-      if constexpr (OWN_KEYS) {
-        team.qmeta[buf].lse2[tt] = r_lse2;
-        team.qmeta[buf].delta[tt] = r_delta;
-        team.qmeta[buf].slope2[tt] = r_slope2;
-      }
+  // The copies of the tile in `buf` are complete, for this wave (those of a newer tile may be in flight); masks need its rows' order.
+  auto arrive = [&](int buf, bool newer, bool part, int n) {
+    if (!newer || !copies) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    else switch (copies - 2 * C::N) {
+      case 0: asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * C::N) : "memory"); break;
+      case 1: asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * C::N + 1) : "memory"); break;
+      case 2: asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * C::N + 2) : "memory"); break;
+      case 3: asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * C::N + 3) : "memory"); break;
+      default: asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * C::N + 4) : "memory"); break;
+    }
+    if (part && tt < ROWS) {
+      RowMeta<ROWS>& meta = team.meta[buf];
+      RowRaw raw = {0.f, 0, tt < n ? 0u : 1u};
+      if (a.causal) raw.pos = meta.pos[tt];
+      if (!OWN_KEYS && a.key_pad && __float_as_uint(meta.order[tt])) raw.pad = 1u;
+      meta.order[tt] = OWN_KEYS ? query_info(a, raw).order : key_info(a, prefix, raw).order;
     }
   };
   // values of a tile with masked pairs that are not finite: 0 in their place, and a mark on their row
@@ -610,10 +634,10 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, ND, WHICH>())) void
 
   // one block of 32 streamed rows; part: with masked pairs
   const LaneAt<T, ND, ROWS> at_lane(lane);
-  auto block = [&](int buf, int row32, bool part) {
+  float tile_slope2 = 0.f;   // of the streamed tile's head
+  auto products = [&](int buf, int row32, f32x16& sc, f32x16& dp) {
     const unsigned ta = lds_at(team.tile[buf][0]), tb = lds_at(team.tile[buf][1]);
-    const RowMeta<ROWS>& meta = team.meta[buf];
-    f32x16 sc = zero16(), dp;
+    sc = zero16();
 #pragma unroll
     for (int st = 0; st < 2 * ND; ++st)
       if (sizeof(T) == 2 || 16 * st < dh) sc = at_lane.rows(ta, row32, st, own1[st], sc, dh - 16 * st);
@@ -623,6 +647,10 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, ND, WHICH>())) void
       for (int st = 0; st < 2 * ND; ++st)
         if (sizeof(T) == 2 || 16 * st < dh) dp = at_lane.rows(tb, row32, st, own2[st], dp, dh - 16 * st);
     }
+  };
+  auto block = [&](int buf, int row32, bool part, const f32x16& sc, const f32x16& dp) {
+    const unsigned ta = lds_at(team.tile[buf][0]), tb = lds_at(team.tile[buf][1]);
+    const RowMeta<ROWS>& meta = team.meta[buf];
     const float k = CAP ? a.cap2 : a.c_in;   // raw score, or tangent, -> score in units of log2
     bool large = false;
     if constexpr (CAP) {
@@ -647,7 +675,7 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, ND, WHICH>())) void
         x[e] = __builtin_fmaf(x[e], k, -ref);
         if constexpr (BIAS) {
           float sl = own_slope2;
-          if constexpr (OWN_KEYS) sl = team.qmeta[buf].slope2[row0 + e];
+          if constexpr (OWN_KEYS) sl = tile_slope2;
           gap[e] = fabsf(meta.pos[row0 + e] - own.pos);
           x[e] = __builtin_fmaf(-sl, gap[e], x[e]);
         }
@@ -657,7 +685,7 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, ND, WHICH>())) void
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const float o = meta.order[row0 + e];
-          const bool sees = (OWN_KEYS ? own.order <= o : o <= own.order) && meta.doc[row0 + e] == own.doc;
+          const bool sees = (OWN_KEYS ? own.order <= o : o <= own.order) && (!docs || meta.doc[row0 + e] == own.doc);
           if (bad && meta.bad[row0 + e] == stamp) x[e] = __builtin_nanf("");
           x[e] = sees ? x[e] : IM_NEG_INF;
         }
@@ -762,7 +790,7 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, ND, WHICH>())) void
       for (int i = wave; i < n; i += CORE_WAVES) {
         const int4 e = lds.list[i];
         const bool in = lane < e.y;
-        const RowInfo info = OWN_KEYS ? query_info(a, b, e.x + lane, in) : key_info(a, b, e.x + lane, in);
+        const RowInfo info = OWN_KEYS ? query_info(a, query_raw(a, b, e.x + lane, in)) : key_info(a, prefix, key_raw(a, b, e.x + lane, in));
         const Range r = range_of(info, in);
         const int cls = OWN_KEYS ? tile_class(mine, r, e.y == ROWS) : tile_class(r, mine, e.y == ROWS);
         if (lane == 0) lds.list[i].z = cls;
@@ -771,28 +799,52 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, ND, WHICH>())) void
     }
     // ---- walk over it ----
     const int step = FEW ? CORE_WAVES : 1;
-    auto next = [&](int i) {
-      while (i < n && lds.list[i].z == TILE_SKIP) i += step;
-      return i;
+    // The copies run BUFS - 1 tiles ahead of the products; queue[0] is the tile at hand.
+    int i = (FEW ? wave : 0) - step;
+    auto next = [&]() {   // the next tile to visit; its row count is 0 at the end
+      int4 e;
+      do {
+        i += step;
+        e = i < n ? lds.list[i] : make_int4(0, 0, TILE_FULL, 0);
+      } while (__builtin_amdgcn_readfirstlane(e.z) == TILE_SKIP);
+      return make_int4(__builtin_amdgcn_readfirstlane(e.x), __builtin_amdgcn_readfirstlane(e.y), __builtin_amdgcn_readfirstlane(e.z),
+                       OWN_KEYS ? __builtin_amdgcn_readfirstlane(e.w) : 0);
     };
-    int i = next(FEW ? wave : 0), buf = 0;
-    if (BUFS == 2 && i < n) fetch(lds.list[i], 0);
-    while (i < n) {
-      const int cls = __builtin_amdgcn_readfirstlane(lds.list[i].z);
-      if (BUFS == 1) fetch(lds.list[i], 0);
-      arrive(buf);
-      team_sync<FEW>();   // all waves' copies are there, and nobody reads the other buffer any more
+    int4 queue[BUFS];
+    int buf = 0;
+#pragma unroll
+    for (int j = 0; j + 1 < BUFS; ++j) {
+      queue[j] = next();
+      if (queue[j].y) fetch(queue[j], j);
+    }
+    if (BUFS == 1) queue[0] = next();
+    while (queue[0].y) {
+      const bool part = queue[0].z == TILE_PART;
+      if (BUFS == 1) fetch(queue[0], 0);
+      arrive(buf, BUFS == 3 && queue[BUFS > 1 ? 1 : 0].y, part, queue[0].y);
+      queue[BUFS - 1] = BUFS > 1 ? next() : queue[0];
+      team_sync<FEW>();   // all waves' copies are there, and nobody reads the oldest buffer any more
       ++stamp;
-      i = next(i + step);
-      if (BUFS == 2 && i < n) fetch(lds.list[i], buf ^ 1);
-      if (cls == TILE_PART) {
+      if (BUFS > 1 && queue[BUFS - 1].y) fetch(queue[BUFS - 1], buf == 0 ? BUFS - 1 : buf - 1);
+      if (part) {
         clean(buf);
         team_sync<FEW>();
       }
+      if constexpr (BIAS && OWN_KEYS) {
+        typedef const float __attribute__((address_space(4))) * const_ptr;   // (a scalar load: no wait for the copies in flight)
+        tile_slope2 = ((const_ptr)(uintptr_t)a.slope)[head0 + queue[0].w] * LOG2E;
+      }
 #pragma unroll
-      for (int r = 0; r < ROWS; r += 32) block(buf, r, cls == TILE_PART);
+      for (int r = 0; r < ROWS / 32; ++r) {
+        f32x16 sc, dp;
+        products(buf, 32 * r, sc, dp);
+        block(buf, 32 * r, part, sc, dp);
+      }
       if constexpr (FEW) team_sync<FEW>();
-      buf ^= BUFS - 1;
+      buf = buf == BUFS - 1 ? 0 : buf + 1;
+#pragma unroll
+      for (int j = 0; j + 1 < BUFS; ++j) queue[j] = queue[j + 1];
+      if (BUFS == 1) queue[0] = next();
     }
     __syncthreads();   // the list is overwritten
   }
