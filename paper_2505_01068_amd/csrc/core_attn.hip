@@ -163,8 +163,18 @@ static void core_args(const im_core_t* s, const im_core_rules_t* r, CoreArgs* a)
   a->Tq = a->q_off[s->n_seg]; a->Tk = a->k_off[s->n_seg];
   a->causal = s->causal != 0;
   a->cap = s->cap;
-  a->cap2 = s->cap * 1.44269504088896340736f;
-  a->c_in = s->cap == 0.f ? s->scale * 1.44269504088896340736f : s->scale / s->cap;
+  if (s->scale == 0.f) a->cap = 0.f;   // every score is 0, capped or not
+  a->to_log2 = s->scale * 1.44269504088896340736f;
+  if (a->cap != 0.f) {
+    const double c = (double)s->scale / s->cap, c2 = c * c;
+    a->c_in = (float)c;
+    a->inv_c_in = (float)(1.0 / c);
+    // coefficients in the raw score; where their powers leave fp32 every score takes the exponential
+    const bool in = c > 1e-5 && c < 1e5;
+    a->small_to = in ? (float)(0.4 / c) : 0.f;
+    const double q[3] = {-0.33331882, 0.13277628, -0.0477942};
+    for (int i = 0; i < 3; ++i) a->tanh_q[i] = in ? (float)(q[i] * pow(c2, i + 1)) : 0.f;
+  }
   a->scale = s->scale;
   if (r) {
     a->valid_len = r->valid_len; a->key_pad = r->key_pad; a->slope = r->slope; a->prefix = r->prefix;

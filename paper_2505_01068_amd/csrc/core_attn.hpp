@@ -15,8 +15,10 @@ struct CoreArgs {
   int splits;                     // workgroups that share the keys of one tile (forward)
   unsigned vec;                   // bit per tensor (VecBit): heads in aligned 16-byte units
   int causal;
-  float c_in;                     // raw score -> argument of the tangent (scale / cap), or scale * log2(e) without a cap
-  float cap, cap2;                // cap and cap * log2(e)
+  float cap;
+  float to_log2;                  // scale * log2(e): raw score (after the cap) -> units of log2
+  float c_in, inv_c_in;           // scale / cap: raw score -> argument of the tangent
+  float small_to, tanh_q[3];      // raw scores below small_to take the polynomial 1 + u (q0 + u (q1 + u q2)), u = raw^2
   float scale;
   im_view_t q, k, v, o, d_o, dq, dk, dv;
   const int32_t* valid_len;

@@ -250,30 +250,30 @@ __device__ __forceinline__ T* head_of(const im_view_t& v, long b, long row, long
 }
 
 // ---- scores ----
-// Hyperbolic tangent of N arguments to fp32 accuracy.  Below 1/2 it is x (1 + u Q(u)), u = x^2, with Q of degree 3 fitted to the
-// smallest relative error there (1.5e-8): 7 multiply-adds, where (1 - e) / (1 + e), e = exp(-2 |x|), takes an exponential and
-// a reciprocal.  Scores rarely come near half of their cap, so the wave looks at its largest argument first (`large`) and
-// takes the exponential only if it has to; an argument gives the same bits either way.
-__device__ __forceinline__ float tanh_small(float x) {
-  const float u = x * x;
-  const float w = __builtin_fmaf(u, __builtin_fmaf(u, __builtin_fmaf(u, __builtin_fmaf(u, 0.01724148f, -0.05304549f), 0.13325879f), -0.33333144f), 1.f);
-  return x * w;
+// The cap, c tanh(s / c).  For |s / c| < 0.4 tanh x is x (1 + u Q(u)), u = x^2, with Q of degree 2 fitted to the smallest relative
+// error there (1.2e-7, two half steps of fp32); the raw product r = s / scale takes the place of x, its powers of scale / c are in the
+// coefficients.  That is 6 multiply-adds, where (1 - e) / (1 + e), e = exp(-2 |x|), takes an exponential and a reciprocal, each four times as
+// long.  Scores rarely come near half of their cap, so a wave looks at its largest one first (`large`) and
+// takes the exponential only if it has to; a score gives the same bits either way.
+__device__ __forceinline__ float tanh_small(const CoreArgs& a, float r) {   // tanh(c_in r) / c_in
+  const float u = r * r;
+  return r * __builtin_fmaf(u, __builtin_fmaf(u, __builtin_fmaf(u, a.tanh_q[2], a.tanh_q[1]), a.tanh_q[0]), 1.f);
 }
 template <int N>
-__device__ __forceinline__ void tanh_of(float (&x)[N], bool large) {
+__device__ __forceinline__ void tanh_of(const CoreArgs& a, float (&x)[N], bool large) {
   if (large) {
 #pragma unroll
     for (int r = 0; r < N; ++r) {
-      const float ax = fabsf(x[r]), e = fast_exp2(-2.f * LOG2E * ax);
-      const float big = __builtin_copysignf((1.f - e) * __builtin_amdgcn_rcpf(1.f + e), x[r]);
-      float small = tanh_small(x[r]);
+      const float ax = fabsf(x[r]), e = fast_exp2(-2.f * LOG2E * a.c_in * ax);
+      const float big = __builtin_copysignf((1.f - e) * __builtin_amdgcn_rcpf(1.f + e) * a.inv_c_in, x[r]);
+      float small = tanh_small(a, x[r]);
       asm("" : "+v"(small));   // both are computed: a choice, no branch per score
-      x[r] = ax >= 0.5f ? big : small;
+      x[r] = ax >= a.small_to ? big : small;
       if ((r & 3) == 3) __builtin_amdgcn_sched_barrier(0);   // few at a time: registers are what limits the waves in flight
     }
   } else {
 #pragma unroll
-    for (int r = 0; r < N; ++r) x[r] = tanh_small(x[r]);
+    for (int r = 0; r < N; ++r) x[r] = tanh_small(a, x[r]);
   }
 }
 
@@ -651,24 +651,25 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, ND, WHICH>())) void
   auto block = [&](int buf, int row32, bool part, const f32x16& sc, const f32x16& dp) {
     const unsigned ta = lds_at(team.tile[buf][0]), tb = lds_at(team.tile[buf][1]);
     const RowMeta<ROWS>& meta = team.meta[buf];
-    const float k = CAP ? a.cap2 : a.c_in;   // raw score, or tangent, -> score in units of log2
+    const float k = a.to_log2;   // raw score (after the cap, if any) -> units of log2
     bool large = false;
+    float top = 0.f;
     if constexpr (CAP) {
-      float top = fabsf(sc[0]);
+      top = fabsf(sc[0]);
 #pragma unroll
       for (int r = 1; r < 16; ++r) top = fmaxf(top, fabsf(sc[r]));
-      large = __any(top * a.c_in >= 0.5f);
+      large = __any(top >= a.small_to);
     }
     // Eight rows at a time: register 8 i + e of a product is streamed row row0 + e.  x: score less the reference (forward) or the row's
     // log-sum-exp (backward), -inf where the pair is masked; g: derivative of the cap; gap: distance.
     auto scores = [&](int i, float (&x)[8], float (&g)[CAP && BWD ? 8 : 1], float (&gap)[BIAS ? 8 : 1]) {
       const int row0 = row32 + 16 * i + 8 * h;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = CAP ? sc[8 * i + e] * a.c_in : sc[8 * i + e];
-      if constexpr (CAP) tanh_of(x, large);
+      for (int e = 0; e < 8; ++e) x[e] = sc[8 * i + e];
+      if constexpr (CAP) tanh_of(a, x, large);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        if constexpr (CAP && BWD) g[e] = __builtin_fmaf(-x[e], x[e], 1.f);
+        if constexpr (CAP && BWD) g[e] = __builtin_fmaf(-x[e] * a.c_in, x[e] * a.c_in, 1.f);
         float ref = m;
         if constexpr (WHICH == CORE_DQ) ref = own_lse2;
         if constexpr (WHICH == CORE_DKV) ref = team.qmeta[buf].lse2[row0 + e];
@@ -696,14 +697,24 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, ND, WHICH>())) void
       float x[2][8], none[1], gap[BIAS ? 8 : 1];
       float mx = IM_NEG_INF;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        scores(i, x[i], none, gap);
+      for (int i = 0; i < 2; ++i) scores(i, x[i], none, gap);
+      auto largest = [&]() {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) mx = fmaxf(mx, x[i][e]);
-      }
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) mx = fmaxf(mx, x[i][e]);
+      };
+      // A cap makes no score larger, nor does a bias by distance unless its slope is negative: |raw score| bounds it, which is known already.
+      constexpr bool BOUND = CAP;
+      if constexpr (BOUND) mx = own_slope2 < 0.f ? __builtin_inff() : __builtin_fmaf(top, k, -m);
+      else largest();
       // A row's reference is its first block's largest score and moves only when a score exceeds it by 8: probabilities stay below
       // 2^8, and no row's bits depend on another's.
       if (__any(mx > most)) {
+        if constexpr (BOUND) {
+          mx = IM_NEG_INF;
+          largest();
+        }
         mx = fmaxf(mx, other_half(mx));
         const float by = mx > most ? mx : 0.f;
         const float f = by > 0.f ? fast_exp2(-by) : 1.f;   // (a first reference below 0 has nothing to scale yet)
@@ -737,12 +748,18 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, ND, WHICH>())) void
           if constexpr (OWN_KEYS) delta = team.qmeta[buf].delta[row0 + e];
           x[e] = fast_exp2(x[e]);
           ds[e] = x[e] * (dp[8 * i + e] - delta);
-          if constexpr (BIAS && WHICH == CORE_DQ) {
-            dslope -= ds[e] * gap[e];
+        }
+        if (BIAS && WHICH == CORE_DQ && a.dslope_rows) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            dslope -= ds[e] * gap[BIAS ? e : 0];
             rest += ds[e];
-            mean_gap += x[e] * gap[e];
+            mean_gap += x[e] * gap[BIAS ? e : 0];
           }
-          if constexpr (CAP) ds[e] *= g[e];
+        }
+        if constexpr (CAP) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) ds[e] *= g[e];
         }
         // A masked pair has x = 0.  Its other factors are finite where keys are streamed (or the owned row's results are lost anyway); an owned
         // key that nobody sees, and the statistics of a query that does not see it, may be anything.
