@@ -88,7 +88,10 @@ static CoreLaunch core_launch(const im_core_t* s, bool own_keys, bool may_split,
     }
     most = std::max(most, work[i]);
   }
-  L.few = t128 * groups < cu_count() || 4 * t128 > 2 * t32;
+#ifndef FEW_MULT
+#define FEW_MULT 1
+#endif
+  L.few = t128 * groups < FEW_MULT * cu_count() || 4 * t128 > 2 * t32;
   const int own = L.few ? 32 : 128;
   L.tiles = (int)(L.few ? t32 : t128);
   L.splits = 1;

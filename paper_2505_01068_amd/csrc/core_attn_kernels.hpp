@@ -144,6 +144,19 @@ __device__ __forceinline__ F8 pack_p(const float*, const float* p) {
 }
 
 // ---- global memory ----
+// The asynchronous copies of mfma_common.hpp with five wait states in front: these kernels have more uniform values than scalar registers,
+// and a base that v_readlane has just brought back must not be read by a memory instruction earlier (the compiler does not look into
+// the statement).
+#define CORE_COPY(NAME, INSTRUCTION)                                                                              \
+  __device__ __forceinline__ void NAME(const void* gbase, unsigned byte_off, const void* lds_wave_base) {         \
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\t" INSTRUCTION " %1, %2"                                         \
+                 :: "s"(lds_offset(lds_wave_base)), "v"(byte_off), "s"(gbase) : "memory");                        \
+  }
+CORE_COPY(copy16, "global_load_lds_dwordx4")
+CORE_COPY(copy4, "global_load_lds_dword")
+CORE_COPY(copy1, "global_load_lds_ubyte")
+#undef CORE_COPY
+
 // 16 bytes from element `at` of a head of dh elements; units at or behind its end give 0
 template <class T>
 __device__ __forceinline__ u32x4 load_unit(const T* head, int at, int dh, bool vec) {
@@ -361,9 +374,7 @@ template <class T, int ND, bool FEW> struct CoreCfg {
   static constexpr int ROWS = FEW || sizeof(T) == 4 ? 32 : 64;      // streamed rows of a tile
   static constexpr int TEAM = FEW ? 64 : 64 * CORE_WAVES;           // threads that load a tile together
   static constexpr int OWN = FEW ? 32 : 32 * CORE_WAVES;            // owned rows of a workgroup
-  // Tiles in LDS.  A workgroup's copies run two tiles ahead where the LDS of two workgroups a CU allows, a wave's on its own one ahead; four
-  // teams' pairs of the widest fp32 tiles do not fit the LDS twice.
-  static constexpr int BUFS = FEW && sizeof(T) == 4 && ND == 4 ? 1 : FEW || ND == 4 ? 2 : 3;
+  static constexpr int BUFS = FEW && sizeof(T) == 4 && ND == 4 ? 1 : 2;   // four teams' pairs of the widest fp32 tiles do not fit the LDS twice
   static constexpr int N = Tile<T, ND, ROWS>::SLOTS / TEAM;         // 16-byte units a thread and tensor
 };
 
@@ -392,8 +403,11 @@ __device__ __forceinline__ void team_sync() {
   } else __syncthreads();
 }
 
-__device__ __forceinline__ bool odd_bits(bf16_t, unsigned u) { return (u & 0x7f80u) == 0x7f80u || (u & 0x7f800000u) == 0x7f800000u; }
-__device__ __forceinline__ bool odd_bits(float, unsigned u) { return (u & 0x7f800000u) == 0x7f800000u; }
+// Exponents that are all ones (infinity, NaN) carry into the sign's place; the bits of other numbers that are added stay below it.
+__device__ __forceinline__ unsigned odd_bits(bf16_t, unsigned u) { return (u & 0x7f807f80u) + 0x00800080u; }
+__device__ __forceinline__ unsigned odd_bits(float, unsigned u) { return (u & 0x7f800000u) + 0x00800000u; }
+__device__ __forceinline__ bool odd(bf16_t, unsigned bits) { return (bits & 0x80008000u) != 0; }
+__device__ __forceinline__ bool odd(float, unsigned bits) { return (bits & 0x80000000u) != 0; }
 __device__ __forceinline__ unsigned clean_bits(bf16_t, unsigned u) {
   if ((u & 0x7f80u) == 0x7f80u) u &= 0xffff0000u;
   if ((u & 0x7f800000u) == 0x7f800000u) u &= 0x0000ffffu;
@@ -428,9 +442,13 @@ __device__ __forceinline__ Place place_of(const CoreArgs& a, int nord) {
 }
 
 // ---- the kernel ----
-// Waves a SIMD: two where the registers of both fit (256 each), one for the widest accumulators.
+// Waves a SIMD that the registers are cut for.  Up to head dimension 64 three (168 registers each) but for dK/dV, whose accumulators are
+// twice as many (two: 8 x 4608 steps, dQ 407 -> 356 us with three); for wider heads two, or one where even 256 registers would spill.
 template <class T, int ND, CoreKernel WHICH>
-constexpr int core_waves() { return ND == 4 && (sizeof(T) == 4 || WHICH == CORE_DKV) ? 1 : 2; }
+constexpr int core_waves() {
+  if (ND == 4) return sizeof(T) == 4 || WHICH == CORE_DKV ? 1 : 2;
+  return WHICH == CORE_DKV || sizeof(T) == 4 ? 2 : 3;
+}
 
 template <class T, int ND, bool FEW, bool CAP, bool BIAS, CoreKernel WHICH>
 __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, ND, WHICH>())) void core_kernel(CoreArgs a) {
@@ -559,7 +577,7 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, ND, WHICH>())) void
           const int u = tt + i * C::TEAM;
           o = (unsigned)(min(TL::row_of(u), n - 1) * view.row * (long)sizeof(T)) + 16 * TL::unit_of(u);
         }
-        if (has[i]) dma16_off(from, o, to + (i * C::TEAM + (FEW ? 0 : wave * 64)) * 16);
+        if (has[i]) copy16(from, o, to + (i * C::TEAM + (FEW ? 0 : wave * 64)) * 16);
       }
     } else {   // element by element, through registers
 #pragma unroll 1
@@ -573,8 +591,6 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, ND, WHICH>())) void
   const int* docs = OWN_KEYS ? a.q_doc : a.k_doc;
   const float* poss = OWN_KEYS ? a.q_pos : a.k_pos;
   const int own_side = OWN_KEYS ? a.Tq : a.Tk;   // (rows of the streamed side)
-  const int n_meta = (FEW || wave == 0) ? (with_pos ? 1 : 0) + (docs ? 1 : 0) + (!OWN_KEYS && a.key_pad ? 1 : 0) + (OWN_KEYS ? 2 : 0) : 0;
-  const int copies = (vec_a && vec_b) ? 2 * C::N + n_meta : 0;   // this wave's copies of a tile in flight; 0: they are waited for at once
   auto fetch = [&](int4 e, int buf) {
     const int row0 = __builtin_amdgcn_readfirstlane(e.x), n = __builtin_amdgcn_readfirstlane(e.y);
     const int g = OWN_KEYS ? __builtin_amdgcn_readfirstlane(e.w) : 0;
@@ -583,26 +599,19 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, ND, WHICH>())) void
     if (tt < ROWS) {
       const unsigned r = (unsigned)min(tt, n - 1);
       const long at0 = (long)b * own_side + row0;
-      if (with_pos) dma4_off(poss + at0, 4 * r, team.meta[buf].pos);
-      if (docs) dma4_off(docs + at0, 4 * r, team.meta[buf].doc);
-      if (!OWN_KEYS && a.key_pad) dma1_off(a.key_pad + at0, r, team.meta[buf].order);
+      if (with_pos) copy4(poss + at0, 4 * r, team.meta[buf].pos);
+      if (docs) copy4(docs + at0, 4 * r, team.meta[buf].doc);
+      if (!OWN_KEYS && a.key_pad) copy1(a.key_pad + at0, r, team.meta[buf].order);
       if constexpr (OWN_KEYS) {
         const long st = ((long)b * a.H + head0 + g) * a.Tq + row0;
-        dma4_off(a.lse2 + st, 4 * r, team.qmeta[buf].lse2);
-        dma4_off(a.delta + st, 4 * r, team.qmeta[buf].delta);
+        copy4(a.lse2 + st, 4 * r, team.qmeta[buf].lse2);
+        copy4(a.delta + st, 4 * r, team.qmeta[buf].delta);
       }
     }
   };
-  // The copies of the tile in `buf` are complete, for this wave (those of a newer tile may be in flight); masks need its rows' order.
-  auto arrive = [&](int buf, bool newer, bool part, int n) {
-    if (!newer || !copies) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    else switch (copies - 2 * C::N) {
-      case 0: asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * C::N) : "memory"); break;
-      case 1: asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * C::N + 1) : "memory"); break;
-      case 2: asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * C::N + 2) : "memory"); break;
-      case 3: asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * C::N + 3) : "memory"); break;
-      default: asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * C::N + 4) : "memory"); break;
-    }
+  // This wave's copies of the tile in `buf` are complete; masks need its rows' order.
+  auto arrive = [&](int buf, bool part, int n) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     if (part && tt < ROWS) {
       RowMeta<ROWS>& meta = team.meta[buf];
       RowRaw raw = {0.f, 0, tt < n ? 0u : 1u};
@@ -614,25 +623,33 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, ND, WHICH>())) void
   // values of a tile with masked pairs that are not finite: 0 in their place, and a mark on their row
   auto clean = [&](int buf) {
     u32x4* units = (u32x4*)team.tile[buf];
+    unsigned bits = 0;
 #pragma unroll
     for (int i = 0; i < 2 * C::N; ++i) {
       const int u = tt + i * C::TEAM;
       if (TL::unit_of(u % TL::SLOTS) * EPC >= 32 * ND) continue;   // half a panel that nothing reads or writes (ND = 1)
+      const u32x4 x = units[u];
+#pragma unroll
+      for (int w = 0; w < 4; ++w) bits |= odd_bits(T(), x[w]);
+    }
+    if (!odd(T(), bits)) return;
+#pragma unroll 1
+    for (int i = 0; i < 2 * C::N; ++i) {
+      const int u = tt + i * C::TEAM;
+      if (TL::unit_of(u % TL::SLOTS) * EPC >= 32 * ND) continue;
       u32x4 x = units[u];
-      bool odd = false;
+      bits = 0;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) odd |= odd_bits(T(), x[w]);
-      if (odd) {
+      for (int w = 0; w < 4; ++w) bits |= odd_bits(T(), x[w]);
+      if (!odd(T(), bits)) continue;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) x[w] = clean_bits(T(), x[w]);
-        units[u] = x;
-        team.meta[buf].bad[TL::row_of(u % TL::SLOTS)] = stamp;
-        team.meta[buf].any_bad = stamp;
-      }
+      for (int w = 0; w < 4; ++w) x[w] = clean_bits(T(), x[w]);
+      units[u] = x;
+      team.meta[buf].bad[TL::row_of(u % TL::SLOTS)] = stamp;
+      team.meta[buf].any_bad = stamp;
     }
   };
 
-  // one block of 32 streamed rows; part: with masked pairs
   const LaneAt<T, ND, ROWS> at_lane(lane);
   float tile_slope2 = 0.f;   // of the streamed tile's head
   auto products = [&](int buf, int row32, f32x16& sc, f32x16& dp) {
@@ -704,9 +721,9 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, ND, WHICH>())) void
 #pragma unroll
           for (int e = 0; e < 8; ++e) mx = fmaxf(mx, x[i][e]);
       };
-      // A cap makes no score larger, nor does a bias by distance unless its slope is negative: |raw score| bounds it, which is known already.
-      constexpr bool BOUND = CAP;
-      if constexpr (BOUND) mx = own_slope2 < 0.f ? __builtin_inff() : __builtin_fmaf(top, k, -m);
+      // A cap makes no score larger: the largest |raw score|, which is known already, bounds it.
+      constexpr bool BOUND = CAP && !BIAS;
+      if constexpr (BOUND) mx = __builtin_fmaf(top, k, -m);
       else largest();
       // A row's reference is its first block's largest score and moves only when a score exceeds it by 8: probabilities stay below
       // 2^8, and no row's bits depend on another's.
@@ -816,7 +833,6 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, ND, WHICH>())) void
     }
     // ---- walk over it ----
     const int step = FEW ? CORE_WAVES : 1;
-    // The copies run BUFS - 1 tiles ahead of the products; queue[0] is the tile at hand.
     int i = (FEW ? wave : 0) - step;
     auto next = [&]() {   // the next tile to visit; its row count is 0 at the end
       int4 e;
@@ -827,29 +843,24 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, ND, WHICH>())) void
       return make_int4(__builtin_amdgcn_readfirstlane(e.x), __builtin_amdgcn_readfirstlane(e.y), __builtin_amdgcn_readfirstlane(e.z),
                        OWN_KEYS ? __builtin_amdgcn_readfirstlane(e.w) : 0);
     };
-    int4 queue[BUFS];
+    int4 e = next();
     int buf = 0;
-#pragma unroll
-    for (int j = 0; j + 1 < BUFS; ++j) {
-      queue[j] = next();
-      if (queue[j].y) fetch(queue[j], j);
-    }
-    if (BUFS == 1) queue[0] = next();
-    while (queue[0].y) {
-      const bool part = queue[0].z == TILE_PART;
-      if (BUFS == 1) fetch(queue[0], 0);
-      arrive(buf, BUFS == 3 && queue[BUFS > 1 ? 1 : 0].y, part, queue[0].y);
-      queue[BUFS - 1] = BUFS > 1 ? next() : queue[0];
-      team_sync<FEW>();   // all waves' copies are there, and nobody reads the oldest buffer any more
+    if (BUFS == 2 && e.y) fetch(e, 0);
+    while (e.y) {
+      const bool part = e.z == TILE_PART;
+      if (BUFS == 1) fetch(e, 0);
+      const int4 ahead = next();
+      arrive(buf, part, e.y);
+      team_sync<FEW>();   // all waves' copies are there, and nobody reads the other buffer any more
       ++stamp;
-      if (BUFS > 1 && queue[BUFS - 1].y) fetch(queue[BUFS - 1], buf == 0 ? BUFS - 1 : buf - 1);
+      if (BUFS == 2 && ahead.y) fetch(ahead, buf ^ 1);
       if (part) {
         clean(buf);
         team_sync<FEW>();
       }
       if constexpr (BIAS && OWN_KEYS) {
         typedef const float __attribute__((address_space(4))) * const_ptr;   // (a scalar load: no wait for the copies in flight)
-        tile_slope2 = ((const_ptr)(uintptr_t)a.slope)[head0 + queue[0].w] * LOG2E;
+        tile_slope2 = ((const_ptr)(uintptr_t)a.slope)[head0 + e.w] * LOG2E;
       }
 #pragma unroll
       for (int r = 0; r < ROWS / 32; ++r) {
@@ -858,10 +869,8 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, ND, WHICH>())) void
         block(buf, 32 * r, part, sc, dp);
       }
       if constexpr (FEW) team_sync<FEW>();
-      buf = buf == BUFS - 1 ? 0 : buf + 1;
-#pragma unroll
-      for (int j = 0; j + 1 < BUFS; ++j) queue[j] = queue[j + 1];
-      if (BUFS == 1) queue[0] = next();
+      buf ^= BUFS - 1;
+      e = ahead;
     }
     __syncthreads();   // the list is overwritten
   }
