@@ -186,8 +186,15 @@ static void core_args(const im_core_t* s, const im_core_rules_t* r, CoreArgs* a)
   }
 }
 
-// Streamed tensors in 16-byte units are addressed by 32-bit byte offsets within a tile of up to 64 rows.
-static unsigned vec_bit(const im_view_t& v, int dh, size_t es, unsigned bit) { return view_in_16s(v, dh, es) && (uint64_t)v.row * es * 64 < (1ull << 32) ? bit : 0u; }
+// Which tensors lie in units of 16 and of 4 bytes.  Streamed ones are addressed by 32-bit byte offsets within a tile of up to 64 rows.
+static void core_units(CoreArgs* a, size_t es) {
+  const im_view_t* views[8] = {&a->q, &a->k, &a->v, &a->o, &a->d_o, &a->dq, &a->dk, &a->dv};
+  for (int i = 0; i < 8; ++i) {
+    if ((uint64_t)views[i]->row * es * 64 >= (1ull << 32)) continue;
+    if (view_in_units(*views[i], a->dh, es, 16)) a->vec |= 1u << i;
+    if (view_in_units(*views[i], a->dh, es, 4)) a->words |= 1u << i;
+  }
+}
 
 struct CoreSizes { size_t o32, saved, part_o, fwd, stat, bwd; };
 static CoreSizes core_sizes(const im_core_t* s) {
@@ -247,8 +254,7 @@ int im_core_attention_fwd(const im_core_t* shape, const im_core_rules_t* rules, 
   const CoreSizes z = core_sizes(shape);
   if (int rc = check_buffer(what, "workspace", workspace, workspace_bytes, z.fwd)) return rc;
   a.q = *q; a.k = *k; a.v = *v; a.o = *o; a.lse = lse;
-  a.vec = vec_bit(a.q, a.dh, es, VEC_Q) | vec_bit(a.k, a.dh, es, VEC_K) | vec_bit(a.v, a.dh, es, VEC_V) |
-          vec_bit(a.o, a.dh, es, VEC_O);
+  core_units(&a, es);
   if (saved) { a.o32 = (float*)saved; a.lse2 = (float*)((char*)saved + z.o32); }
   a.part_o = (float*)workspace; a.part_ml = (float*)((char*)workspace + z.part_o);
   const CoreLaunch L = core_launch(shape, false, true, &a);
@@ -290,9 +296,7 @@ int im_core_attention_bwd(const im_core_t* shape, const im_core_rules_t* rules, 
   if ((uintptr_t)saved % 16) return refuse(IM_ERR_INVALID, "%s: saved must be 16-byte aligned", what);
   if (int rc = check_buffer(what, "workspace", workspace, workspace_bytes, z.bwd)) return rc;
   a.q = *q; a.k = *k; a.v = *v; a.d_o = *d_o; a.dq = *dq; a.dk = *dk; a.dv = *dv;
-  a.vec = vec_bit(a.q, a.dh, es, VEC_Q) | vec_bit(a.k, a.dh, es, VEC_K) | vec_bit(a.v, a.dh, es, VEC_V) |
-          vec_bit(a.d_o, a.dh, es, VEC_DO) | vec_bit(a.dq, a.dh, es, VEC_DQ) | vec_bit(a.dk, a.dh, es, VEC_DK) |
-          vec_bit(a.dv, a.dh, es, VEC_DV);
+  core_units(&a, es);
   a.o32 = (float*)saved; a.lse2 = (float*)((char*)saved + z.o32);
   a.delta = (float*)workspace;
   a.dslope_rows = dslope ? (float*)((char*)workspace + z.stat) : nullptr;

@@ -13,7 +13,7 @@ struct CoreArgs {
   // tiles of the kernel's own rows: segments in launch order, those with most to read first
   int order[IM_MAX_SEG], tile_prefix[IM_MAX_SEG + 1];
   int splits;                     // workgroups that share the keys of one tile (forward)
-  unsigned vec;                   // bit per tensor (VecBit): heads in aligned 16-byte units
+  unsigned vec, words;            // bit per tensor (VecBit): heads in aligned units of 16 bytes, of 4 bytes
   int causal;
   float cap;
   float to_log2;                  // scale * log2(e): raw score (after the cap) -> units of log2

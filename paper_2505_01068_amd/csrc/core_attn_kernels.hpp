@@ -529,6 +529,7 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, ND, WHICH>())) void
   const int head0 = OWN_KEYS ? at.kvh * a.G : at.kvh;
   const T *base_a = head_of<const T>(va, b, 0, head0), *base_b = head_of<const T>(vb, b, 0, head0);
   const bool vec_a = a.vec & (OWN_KEYS ? VEC_Q : VEC_K), vec_b = a.vec & (OWN_KEYS ? VEC_DO : VEC_V);
+  const bool words_a = a.words & (OWN_KEYS ? VEC_Q : VEC_K), words_b = a.words & (OWN_KEYS ? VEC_DO : VEC_V);
   const unsigned live = OWN_KEYS ? a.k_live[at.seg] : a.q_live[at.seg];
   const bool scan = a.causal || a.q_doc || (a.key_pad && !OWN_KEYS);   // classes that depend on the streamed rows' data
   auto stream_len = [&](int j) {   // rows of streamed segment j that count
@@ -568,7 +569,7 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, ND, WHICH>())) void
   }
   int stamp = 0;
   // one tensor's tile; rows behind the n-th repeat the last one (no pair of theirs counts)
-  auto copy = [&](const T* from, const im_view_t& view, const unsigned (&off)[C::N], bool vec, char* to, int n) {
+  auto copy = [&](const T* from, const im_view_t& view, const unsigned (&off)[C::N], bool vec, bool words, char* to, int n) {
     if (vec) {
 #pragma unroll
       for (int i = 0; i < C::N; ++i) {
@@ -578,6 +579,13 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, ND, WHICH>())) void
           o = (unsigned)(min(TL::row_of(u), n - 1) * view.row * (long)sizeof(T)) + 16 * TL::unit_of(u);
         }
         if (has[i]) copy16(from, o, to + (i * C::TEAM + (FEW ? 0 : wave * 64)) * 16);
+      }
+    } else if (words) {   // 4 bytes a lane
+#pragma unroll(C::N > 2 ? 2 : 4)
+      for (int i = 0; i < 4 * C::N; ++i) {
+        const int w = tt + i * C::TEAM, at = 16 * TL::unit_of(w >> 2) + 4 * (w & 3);
+        const unsigned o = (unsigned)min(TL::row_of(w >> 2), n - 1) * (unsigned)(view.row * (long)sizeof(T)) + at;
+        if (at < dh * (int)sizeof(T)) copy4(from, o, to + (i * C::TEAM + (FEW ? 0 : wave * 64)) * 4);
       }
     } else {   // element by element, through registers
 #pragma unroll 1
@@ -594,8 +602,8 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, ND, WHICH>())) void
   auto fetch = [&](int4 e, int buf) {
     const int row0 = __builtin_amdgcn_readfirstlane(e.x), n = __builtin_amdgcn_readfirstlane(e.y);
     const int g = OWN_KEYS ? __builtin_amdgcn_readfirstlane(e.w) : 0;
-    copy(base_a + row0 * va.row + g * va.head, va, off_a, vec_a, team.tile[buf][0], n);
-    copy(base_b + row0 * vb.row + g * vb.head, vb, off_b, vec_b, team.tile[buf][1], n);
+    copy(base_a + row0 * va.row + g * va.head, va, off_a, vec_a, words_a, team.tile[buf][0], n);
+    copy(base_b + row0 * vb.row + g * vb.head, vb, off_b, vec_b, words_b, team.tile[buf][1], n);
     if (tt < ROWS) {
       const unsigned r = (unsigned)min(tt, n - 1);
       const long at0 = (long)b * own_side + row0;

@@ -32,9 +32,9 @@ inline int check_view(const char* what, const char* name, const im_view_t* v, co
   return IM_OK;
 }
 
-// whether every head of the view starts on 16 bytes and is whole 16-byte units long
-inline bool view_in_16s(const im_view_t& v, int head_dim, size_t es) {
-  return (uintptr_t)v.ptr % 16 == 0 && head_dim * es % 16 == 0 && v.batch * es % 16 == 0 && v.row * es % 16 == 0 && v.head * es % 16 == 0;
+// whether every head of the view starts on a multiple of `unit` bytes and is whole units long
+inline bool view_in_units(const im_view_t& v, int head_dim, size_t es, size_t unit) {
+  return (uintptr_t)v.ptr % unit == 0 && head_dim * es % unit == 0 && v.batch * es % unit == 0 && v.row * es % unit == 0 && v.head * es % unit == 0;
 }
 
 }  // namespace imattn

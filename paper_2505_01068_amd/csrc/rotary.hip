@@ -185,10 +185,10 @@ extern "C" int im_rotary_apply(const im_rotary_t* s, const float* pos, int64_t p
   a.rows = s->rows; a.n_axes = s->n_axes; a.P = (int)P; a.dh = s->head_dim; a.qh = s->q_heads; a.kh = s->k_heads; a.inverse = s->inverse != 0;
   a.pos = pos; a.pos_batch = pos_batch; a.inv_freq = inv_freq;
   a.q = *q; a.qo = *q_out;
-  bool in16 = view_in_16s(a.q, a.dh, es) && view_in_16s(a.qo, a.dh, es);
+  bool in16 = view_in_units(a.q, a.dh, es, 16) && view_in_units(a.qo, a.dh, es, 16);
   if (s->k_heads) {
     a.k = *k; a.ko = *k_out;
-    in16 = in16 && view_in_16s(a.k, a.dh, es) && view_in_16s(a.ko, a.dh, es);
+    in16 = in16 && view_in_units(a.k, a.dh, es, 16) && view_in_units(a.ko, a.dh, es, 16);
   }
   hipStream_t st = (hipStream_t)hip_stream;
   ProfScope ps(PF_MISC, st);
