@@ -103,15 +103,35 @@ struct LaneAt<bf16_t, ND, ROWS> {
     return mfma32(lds_frag_tr_at(tile + col[db & 1][0], tile + col[db & 1][1], (db >> 1) * ROWS * 128 + row16 * 128), p, c);
   }
 };
+// a and b with the odd rows of 16 lanes of a and the even ones of b exchanged
+__device__ __forceinline__ u32x2 swap16(float a, float b) {
+  const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+  return u32x2{s[0], s[1]};
+}
 template <int ND, int ROWS>
 struct LaneAt<float, ND, ROWS> {
-  unsigned row[4], col[8];
+  unsigned row[4], col[8], col16[4];
   __device__ __forceinline__ LaneAt(int lane) {
     const int r = perm32(lane & 31), h = lane >> 5;
 #pragma unroll
     for (int i = 0; i < 4; ++i) row[i] = r * ND * 128 + (((2 * i + h) ^ (r & 7)) << 4);
 #pragma unroll
     for (int j = 0; j < 8; ++j) col[j] = (8 * h + j) * ND * 128 + (((r >> 2) ^ j) << 4) + 4 * (r & 3);
+    const int g = (lane >> 4) & 1, c = lane & 15;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) col16[j] = (8 * h + 2 * j + g) * ND * 128 + (((c >> 2) ^ (2 * j + g)) << 4) + 4 * (c & 3);
+  }
+  // Heads of up to 16 elements: the second product on 16 x 16 x 4, half of whose time 16 of 32 columns would waste on 32 x 32 x 2.  c[x]: columns
+  // 16 x .. + 15 of the owned rows.  Exchanging rows of 16 lanes between the probabilities of two streamed rows gives each of the two products
+  // four streamed rows: lanes 16 g .. + 15 hold row 8 (g / 2) + e + g % 2 of the 16-row block.
+  __device__ __forceinline__ void cols16(unsigned tile, int row16, const F8& p, f32x4 (&c)[2]) const {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float v = lds_load<float>(tile + col16[j], row16 * ND * 128);
+      const u32x2 s = swap16(p.v[2 * j], p.v[2 * j + 1]);
+      c[0] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, __uint_as_float(s[0]), c[0], 0, 0, 0);
+      c[1] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, __uint_as_float(s[1]), c[1], 0, 0, 0);
+    }
   }
   __device__ __forceinline__ f32x16 rows(unsigned tile, int row32, int s, const F8& own, f32x16 c, int left) const {   // left: elements from this step on
     const int off = (s >> 1) * 128 + row32 * ND * 128;
@@ -351,7 +371,7 @@ __device__ __forceinline__ void range_wave(Range& r) {
   }
 }
 // rows in range but without a valid order (padding) clear `all`
-__device__ __forceinline__ Range range_of(const RowInfo& i, bool in_range) {
+__device__ __forceinline__ Range range_of(const RowInfo& i, bool in_range, bool numbers) {   // numbers: more than any and all is asked for
   const bool ok = in_range && i.order == i.order;
   Range r;
   r.lo = ok ? i.order : __builtin_inff();
@@ -360,18 +380,21 @@ __device__ __forceinline__ Range range_of(const RowInfo& i, bool in_range) {
   r.dhi = ok ? i.doc : (int)0x80000000;
   r.any = __any(ok);
   r.all = __all(ok || !in_range);
-  range_wave(r);
+  if (numbers) range_wave(r);
   return r;
 }
-__device__ __forceinline__ int tile_class(const Range& keys, const Range& queries, bool whole) {
+__device__ __forceinline__ int tile_class(const Range& keys, const Range& queries, bool whole, bool numbers) {
   if (!keys.any || !queries.any) return TILE_SKIP;
-  if (keys.lo > queries.hi || keys.dlo > queries.dhi || keys.dhi < queries.dlo) return TILE_SKIP;
-  const bool full = whole && keys.all && queries.all && keys.hi <= queries.lo && keys.dlo == keys.dhi && queries.dlo == queries.dhi && keys.dlo == queries.dlo;
+  bool full = whole && keys.all && queries.all;
+  if (numbers) {
+    if (keys.lo > queries.hi || keys.dlo > queries.dhi || keys.dhi < queries.dlo) return TILE_SKIP;
+    full = full && keys.hi <= queries.lo && keys.dlo == keys.dhi && queries.dlo == queries.dhi && keys.dlo == queries.dlo;
+  }
   return full ? TILE_FULL : TILE_PART;
 }
 
 template <class T, int ND, bool FEW> struct CoreCfg {
-  static constexpr int ROWS = FEW || sizeof(T) == 4 ? 32 : 64;      // streamed rows of a tile
+  static constexpr int ROWS = FEW || (sizeof(T) == 4 && ND == 4) ? 32 : 64;   // streamed rows of a tile
   static constexpr int TEAM = FEW ? 64 : 64 * CORE_WAVES;           // threads that load a tile together
   static constexpr int OWN = FEW ? 32 : 32 * CORE_WAVES;            // owned rows of a workgroup
   static constexpr int BUFS = FEW && sizeof(T) == 4 && ND == 4 ? 1 : 2;   // four teams' pairs of the widest fp32 tiles do not fit the LDS twice
@@ -450,14 +473,18 @@ constexpr int core_waves() {
   return WHICH == CORE_DKV || sizeof(T) == 4 ? 2 : 3;
 }
 
-template <class T, int ND, bool FEW, bool CAP, bool BIAS, CoreKernel WHICH>
-__global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, ND, WHICH>())) void core_kernel(CoreArgs a) {
+// W: head width in units of 32 elements, 0 for fp32 heads of up to 16
+template <class T, int W, bool FEW, bool CAP, bool BIAS, CoreKernel WHICH>
+__global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>())) void core_kernel(CoreArgs a) {
+  constexpr int ND = W ? W : 1;
+  constexpr bool NARROW = W == 0;
+  static_assert(!NARROW || sizeof(T) == 4, "");
   using C = CoreCfg<T, ND, FEW>;
   using Frag = typename CoreT<T>::Frag;
   using TL = Tile<T, ND, C::ROWS>;
   constexpr int ROWS = C::ROWS, EPC = CoreT<T>::EPC, BUFS = C::BUFS;
   constexpr bool OWN_KEYS = WHICH == CORE_DKV, BWD = WHICH != CORE_FWD;
-  extern __shared__ __align__(16) char lds_raw[];
+  extern __shared__ __align__(16) char lds_raw[];   // (nothing but the list and the owned rows' ranges outlives the walk over the tiles)
   auto& lds = *(CoreLds<T, ND, FEW, WHICH>*)lds_raw;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), h = lane >> 5;
   const int tt = FEW ? lane : (int)threadIdx.x;     // thread of the team
@@ -498,8 +525,9 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, ND, WHICH>())) void
   }
 
   // ---- range of the owned rows, over the workgroup ----
+  const bool ranges = a.causal || a.q_doc;   // without them every row's order and document are the same
   {
-    const Range r = range_of(own, in_range);
+    const Range r = range_of(own, in_range, ranges);
     if (lane == 0) lds.own[wave] = r;
 #pragma unroll
     for (int i = 0; i < BUFS; ++i) {
@@ -550,6 +578,7 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, ND, WHICH>())) void
     acc1[d] = zero16();
     if constexpr (WHICH == CORE_DKV) acc2[d] = zero16();
   }
+  f32x4 nar1[2] = {}, nar2[2] = {};   // the same of narrow heads
   constexpr float LOWEST = -3.402823466e38f;
   float m = 0.f, l = 0.f, most = LOWEST;   // reference, sum, and by how much a score may exceed the reference
   // A slope's gradient is -sum dS gap.  delta stems from a forward that rounded its probabilities; by how much it is off is what
@@ -750,10 +779,16 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, ND, WHICH>())) void
         for (int i = 0; i < 2; ++i)
 #pragma unroll
           for (int e = 0; e < 8; ++e) x[i][e] -= by;
+        if constexpr (NARROW) {
+          const u32x2 s = swap16(f, f);
+          nar1[0] *= __uint_as_float(s[0]);
+          nar1[1] *= __uint_as_float(s[1]);
+        } else {
 #pragma unroll
-        for (int d = 0; d < ND; ++d)
+          for (int d = 0; d < ND; ++d)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) acc1[d][r] *= f;
+            for (int r = 0; r < 16; ++r) acc1[d][r] *= f;
+        }
       }
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
@@ -796,7 +831,15 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, ND, WHICH>())) void
         q[i] = pack_p((const T*)nullptr, ds);
       }
     }
-    // 32 columns of the second products; WHICH == CORE_DKV: both
+    // the second product; for dK/dV both
+    if constexpr (NARROW) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        if constexpr (WHICH == CORE_FWD) at_lane.cols16(tb, row32 + 16 * i, p[i], nar1);
+        else at_lane.cols16(ta, row32 + 16 * i, q[i], nar1);
+        if constexpr (WHICH == CORE_DKV) at_lane.cols16(tb, row32 + 16 * i, p[i], nar2);
+      }
+    } else
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -833,8 +876,8 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, ND, WHICH>())) void
         const int4 e = lds.list[i];
         const bool in = lane < e.y;
         const RowInfo info = OWN_KEYS ? query_info(a, query_raw(a, b, e.x + lane, in)) : key_info(a, prefix, key_raw(a, b, e.x + lane, in));
-        const Range r = range_of(info, in);
-        const int cls = OWN_KEYS ? tile_class(mine, r, e.y == ROWS) : tile_class(r, mine, e.y == ROWS);
+        const Range r = range_of(info, in, ranges);
+        const int cls = OWN_KEYS ? tile_class(mine, r, e.y == ROWS, ranges) : tile_class(r, mine, e.y == ROWS, ranges);
         if (lane == 0) lds.list[i].z = cls;
       }
       __syncthreads();
@@ -884,6 +927,21 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, ND, WHICH>())) void
   }
 
   // ---- results ----
+  if constexpr (NARROW) {
+    // to the layout of the wide accumulators, through LDS of the wave: lane (n, g) holds elements 4 g .. + 3 of owned rows n and 16 + n
+    float* mine16 = (float*)lds_raw + wave * 32 * 16;
+    auto widen = [&](const f32x4 (&from)[2], f32x16& to) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x) *(f32x4*)(mine16 + (16 * x + (lane & 15)) * 16 + 4 * (lane >> 4)) = from[x];
+      team_sync<true>();
+#pragma unroll
+      for (int r = 0; r < 8; ++r) to[r] = mine16[(lane & 31) * 16 + 8 * h + r];
+      team_sync<true>();
+    };
+    widen(nar1, acc1[0]);
+    if constexpr (WHICH == CORE_DKV) widen(nar2, acc2[0]);
+    __syncthreads();
+  }
   if constexpr (WHICH == CORE_FWD) {
     l += other_half(l);
     if (most == LOWEST) m = LOWEST;   // nothing seen
@@ -973,32 +1031,33 @@ constexpr size_t core_lds() {
   static_assert((need > box ? need : box) <= 160 * 1024, "LDS of a CU");
   return need > box ? need : box;
 }
-template <class T, int ND, bool FEW, bool CAP, bool BIAS, CoreKernel WHICH>
+template <class T, int W, bool FEW, bool CAP, bool BIAS, CoreKernel WHICH>
 static void core_go(const CoreArgs& a, unsigned grid, hipStream_t st) {
-  constexpr size_t lds = core_lds<T, ND, FEW, WHICH>();
-  auto* fn = core_kernel<T, ND, FEW, CAP, BIAS, WHICH>;
+  constexpr size_t lds = core_lds<T, (W ? W : 1), FEW, WHICH>();
+  auto* fn = core_kernel<T, W, FEW, CAP, BIAS, WHICH>;
   if (lds > 64 * 1024) (void)hipFuncSetAttribute((const void*)fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   hipLaunchKernelGGL(fn, dim3(grid), dim3(64 * CORE_WAVES), lds, st, a);
 }
-template <class T, int ND, bool FEW, CoreKernel WHICH>
+template <class T, int W, bool FEW, CoreKernel WHICH>
 static void core_mods(const CoreArgs& a, unsigned grid, hipStream_t st) {
   const bool cap = a.cap > 0.f, bias = a.slope != nullptr;
-  if (cap && bias) core_go<T, ND, FEW, true, true, WHICH>(a, grid, st);
-  else if (cap) core_go<T, ND, FEW, true, false, WHICH>(a, grid, st);
-  else if (bias) core_go<T, ND, FEW, false, true, WHICH>(a, grid, st);
-  else core_go<T, ND, FEW, false, false, WHICH>(a, grid, st);
+  if (cap && bias) core_go<T, W, FEW, true, true, WHICH>(a, grid, st);
+  else if (cap) core_go<T, W, FEW, true, false, WHICH>(a, grid, st);
+  else if (bias) core_go<T, W, FEW, false, true, WHICH>(a, grid, st);
+  else core_go<T, W, FEW, false, false, WHICH>(a, grid, st);
+}
+template <class T, bool FEW, CoreKernel WHICH>
+static void core_width(const CoreArgs& a, unsigned grid, hipStream_t st) {
+  if constexpr (sizeof(T) == 4)
+    if (a.dh <= 16) { core_mods<T, 0, FEW, WHICH>(a, grid, st); return; }
+  if (a.dh <= 32) core_mods<T, 1, FEW, WHICH>(a, grid, st);
+  else if (a.dh <= 64) core_mods<T, 2, FEW, WHICH>(a, grid, st);
+  else core_mods<T, 4, FEW, WHICH>(a, grid, st);
 }
 template <class T, CoreKernel WHICH>
 static void core_widths(bool few, const CoreArgs& a, unsigned grid, hipStream_t st) {
-  if (few) {
-    if (a.dh <= 32) core_mods<T, 1, true, WHICH>(a, grid, st);
-    else if (a.dh <= 64) core_mods<T, 2, true, WHICH>(a, grid, st);
-    else core_mods<T, 4, true, WHICH>(a, grid, st);
-  } else {
-    if (a.dh <= 32) core_mods<T, 1, false, WHICH>(a, grid, st);
-    else if (a.dh <= 64) core_mods<T, 2, false, WHICH>(a, grid, st);
-    else core_mods<T, 4, false, WHICH>(a, grid, st);
-  }
+  if (few) core_width<T, true, WHICH>(a, grid, st);
+  else core_width<T, false, WHICH>(a, grid, st);
 }
 
 }  // namespace imattn
