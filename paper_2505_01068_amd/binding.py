@@ -320,8 +320,10 @@ def gsit_model_fwd(shape, model, x, valid_len=None, key_pad=None, out=None, work
 
 
 # ---- operators around the attention of a layer ----
+# (Small calls are bound by the host: the checks below touch each tensor once and build no containers.)
 
 _DTYPES = {torch.float32: IM_DTYPE_F32, torch.bfloat16: IM_DTYPE_BF16, "fp32": IM_DTYPE_F32, "bf16": IM_DTYPE_BF16}
+_TORCH_TYPES = (torch.float32, torch.bfloat16)
 
 
 def _dtype(t):
@@ -330,51 +332,69 @@ def _dtype(t):
     return _DTYPES[t]
 
 
-def _on_device(device, what, **tensors):
-    """The call goes to the current device's current stream: every tensor has to live on that device."""
-    if device.type != "cuda" or device.index != torch.cuda.current_device():
-        raise ValueError(f"{what}: tensors must be on the current GPU (cuda:{torch.cuda.current_device()}), got {device}")
-    for name, t in tensors.items():
-        if t is not None and t.device != device:
-            raise ValueError(f"{what}: {name} is on {t.device}, not on {device}")
+def _device(what, x):
+    """The call goes to the current device's current stream: every tensor has to live on that device.  Its index."""
+    i = x.get_device()
+    if i < 0 or i != torch.cuda.current_device():
+        raise ValueError(f"{what}: tensors must be on the current GPU, got {x.device}")
+    return i
 
 
-def _want(what, name, t, shape, dtype, optional=False):
-    """A dense tensor of that shape and dtype; None only where it is optional."""
+def _raw_stream(device):
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
+def _want(what, name, t, shape, dtype, device):
+    """Address of a dense tensor of that shape and type; None stays None."""
     if t is None:
-        if optional:
-            return
+        return None
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != device:
+        raise ValueError(f"{what}: {name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on cuda:{device}, got {t.dtype} "
+                         f"{tuple(t.shape)} with strides {t.stride()} on {t.device}")
+    return t.data_ptr()
+
+
+def _needed(what, name, t):
+    if t is None:
         raise ValueError(f"{what}: {name} is needed")
-    if t.shape != shape or t.dtype != dtype or not t.is_contiguous():
-        raise ValueError(f"{what}: {name} must be a contiguous {dtype} tensor of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)} "
-                         f"with strides {t.stride()}")
 
 
-def _want_bytes(what, name, t):
+def _bytes(what, name, t, device, need=0):
+    """(address, bytes) of a uint8 buffer"""
     if t is None:
         return None, 0
-    if t.dtype != torch.uint8 or not t.is_contiguous():
-        raise ValueError(f"{what}: {name} must be a contiguous uint8 tensor")
-    return C.c_void_p(t.data_ptr()), t.numel()
+    if t.dtype is not torch.uint8 or not t.is_contiguous() or t.get_device() != device:
+        raise ValueError(f"{what}: {name} must be a contiguous uint8 tensor on cuda:{device}")
+    if t.numel() < need:
+        raise ValueError(f"{what}: {name} has {t.numel()} bytes, {need} are needed")
+    return t.data_ptr(), t.numel()
 
 
 def _rows(what, name, t, d, dtype, n=None):
     """(rows, distance) of a tensor [..., d] whose rows lie at one distance from each other."""
-    if t.dim() < 1 or t.shape[-1] != d or t.dtype != dtype or (d > 1 and t.stride(-1) != 1):
-        raise ValueError(f"{what}: {name} must be a {dtype} tensor [..., {d}] with its last dimension dense, got {t.dtype} {tuple(t.shape)} "
-                         f"with strides {t.stride()}")
+    shape, stride = t.shape, t.stride()
+    if len(shape) < 1 or shape[-1] != d or t.dtype is not dtype or (d > 1 and stride[-1] != 1):
+        raise ValueError(f"{what}: {name} must be a {dtype} tensor [..., {d}] with its last dimension dense, got {t.dtype} {tuple(shape)} "
+                         f"with strides {stride}")
     rows, ld = 1, 0
-    for size, stride in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
-        if size == 1:
-            continue
-        if rows == 1:
-            ld = stride
-        elif stride != ld * rows:
-            raise ValueError(f"{what}: the rows of {name} must lie at one distance from each other, got shape {tuple(t.shape)} with strides {t.stride()}")
-        rows *= size
+    for i in range(len(shape) - 2, -1, -1):
+        if shape[i] != 1:
+            if rows == 1:
+                ld = stride[i]
+            elif stride[i] != ld * rows:
+                raise ValueError(f"{what}: the rows of {name} must lie at one distance from each other, got shape {tuple(shape)} with strides {stride}")
+            rows *= shape[i]
     if n is not None and rows != n:
         raise ValueError(f"{what}: {name} has {rows} rows, {n} are needed")
     return rows, ld if rows > 1 else d
+
+
+def _row_stat(what, name, t, rows, device):
+    if t is None:
+        return None
+    if t.dtype is not torch.float32 or t.numel() != rows or not t.is_contiguous() or t.get_device() != device:
+        raise ValueError(f"{what}: {name} must be a contiguous float32 tensor of {rows} elements on cuda:{device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
 
 
 def im_layernorm_sizes(rows, d, dtype):
@@ -388,45 +408,49 @@ def im_layernorm_fwd(x, gamma=None, beta=None, eps=1e-5, y=None, mean=None, rstd
     """y = layer norm of x [..., d] over its last dimension, rows at one distance.  mean, rstd: fp32 tensors with one element a
     row that the backward needs, or None for inference.  y may be x."""
     what = "im_layernorm_fwd"
-    y = torch.empty_like(x) if y is None else y
-    _on_device(x.device, what, gamma=gamma, beta=beta, y=y, mean=mean, rstd=rstd)
-    d = x.shape[-1]
-    rows, ldx = _rows(what, "x", x, d, x.dtype)
-    _, ldy = _rows(what, "y", y, d, x.dtype, rows)
-    for name, t in (("gamma", gamma), ("beta", beta)):
-        _want(what, name, t, (d,), x.dtype, True)
-    for name, t in (("mean", mean), ("rstd", rstd)):
-        if t is not None:
-            _want(what, name, t.view(-1), (rows,), torch.float32)
-    _check(lib().im_layernorm_fwd(rows, d, _dtype(x.dtype), _p(x), ldx, _p(gamma), _p(beta), float(eps), _p(y), ldy, _p(mean), _p(rstd),
-                                  _stream()))
+    dev = _device(what, x)
+    if y is None:
+        y = torch.empty_like(x)
+    elif y.get_device() != dev:
+        raise ValueError(f"{what}: y is on {y.device}, not on cuda:{dev}")
+    d, dt = x.shape[-1], x.dtype
+    rows, ldx = _rows(what, "x", x, d, dt)
+    _, ldy = _rows(what, "y", y, d, dt, rows)
+    _check((_lib or lib()).im_layernorm_fwd(rows, d, _dtype(dt), x.data_ptr(), ldx, _want(what, "gamma", gamma, (d,), dt, dev),
+                                            _want(what, "beta", beta, (d,), dt, dev), eps, y.data_ptr(), ldy,
+                                            _row_stat(what, "mean", mean, rows, dev), _row_stat(what, "rstd", rstd, rows, dev), _raw_stream(dev)))
     return y
 
 
 def im_layernorm_bwd(x, gamma, mean, rstd, dy, dx=None, dgamma=None, dbeta=None, workspace=None):
     """Gradients of im_layernorm_fwd into those of dx [..., d], dgamma and dbeta (fp32 [d]) that are given.  dx may be dy."""
     what = "im_layernorm_bwd"
-    _on_device(x.device, what, gamma=gamma, mean=mean, rstd=rstd, dy=dy, dx=dx, dgamma=dgamma, dbeta=dbeta, workspace=workspace)
-    d = x.shape[-1]
-    rows, ldx = _rows(what, "x", x, d, x.dtype)
-    _, lddy = _rows(what, "dy", dy, d, x.dtype, rows)
-    lddx = _rows(what, "dx", dx, d, x.dtype, rows)[1] if dx is not None else 0
-    _want(what, "gamma", gamma, (d,), x.dtype, True)
-    for name, t in (("mean", mean), ("rstd", rstd)):
-        _want(what, name, t if t is None else t.view(-1), (rows,), torch.float32)
-    for name, t in (("dgamma", dgamma), ("dbeta", dbeta)):
-        _want(what, name, t, (d,), torch.float32, True)
-    ws, nbytes = _want_bytes(what, "workspace", workspace)
-    _check(lib().im_layernorm_bwd(rows, d, _dtype(x.dtype), _p(x), ldx, _p(gamma), _p(mean), _p(rstd), _p(dy), lddy, _p(dx), lddx, _p(dgamma),
-                                  _p(dbeta), ws, nbytes, _stream()))
+    dev = _device(what, x)
+    if dy.get_device() != dev or (dx is not None and dx.get_device() != dev):
+        raise ValueError(f"{what}: dy and dx must be on cuda:{dev}")
+    d, dt = x.shape[-1], x.dtype
+    rows, ldx = _rows(what, "x", x, d, dt)
+    _, lddy = _rows(what, "dy", dy, d, dt, rows)
+    lddx = _rows(what, "dx", dx, d, dt, rows)[1] if dx is not None else 0
+    _needed(what, "mean", mean)
+    _needed(what, "rstd", rstd)
+    ws, nbytes = _bytes(what, "workspace", workspace, dev)
+    f32 = torch.float32
+    _check((_lib or lib()).im_layernorm_bwd(rows, d, _dtype(dt), x.data_ptr(), ldx, _want(what, "gamma", gamma, (d,), dt, dev),
+                                            _row_stat(what, "mean", mean, rows, dev), _row_stat(what, "rstd", rstd, rows, dev), dy.data_ptr(), lddy,
+                                            None if dx is None else dx.data_ptr(), lddx, _want(what, "dgamma", dgamma, (d,), f32, dev),
+                                            _want(what, "dbeta", dbeta, (d,), f32, dev), ws, nbytes, _raw_stream(dev)))
     return dx
 
 
-def _view(what, name, t, shape, dtype):
-    if t is None or t.shape != shape or t.dtype != dtype or (shape[3] > 1 and t.stride(3) != 1):
-        got = "None" if t is None else f"{t.dtype} {tuple(t.shape)} with strides {t.stride()}"
-        raise ValueError(f"{what}: {name} must be a {dtype} tensor of shape {tuple(shape)} with dense heads, got {got}")
-    return ImView(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+def _view(what, name, t, shape, dtype, device=None):
+    if t is None or t.dtype is not dtype or t.shape != shape or (device is not None and t.get_device() != device):
+        got = "None" if t is None else f"{t.dtype} {tuple(t.shape)} on {t.device}"
+        raise ValueError(f"{what}: {name} must be a {dtype} tensor of shape {tuple(shape)} on the current GPU, got {got}")
+    b, r, h, e = t.stride()
+    if e != 1 and shape[3] > 1:
+        raise ValueError(f"{what}: the heads of {name} must be dense, got strides {t.stride()}")
+    return ImView(t.data_ptr(), b, r, h)
 
 
 def im_rotary(pos, inv_freq, pairs, q, k=None, q_out=None, k_out=None, interleaved=False, inverse=False):
@@ -434,28 +458,31 @@ def im_rotary(pos, inv_freq, pairs, q, k=None, q_out=None, k_out=None, interleav
     pos: fp32 [B, T, axes], or [T, axes] for all batch elements; pairs: rotated pairs of each axis; inv_freq: fp32
     [sum of pairs].  inverse: the gradient's rotation.  q_out / k_out may be q / k.  Returns (q_out, k_out)."""
     what = "im_rotary"
+    dev = _device(what, q)
     if q.dim() != 4 or (k is not None and k.dim() != 4):
         raise ValueError(f"{what}: q and k must be [batch, rows, heads, head_dim]")
-    q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
-    if k is not None and k_out is None:
-        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
-    _on_device(q.device, what, pos=pos, inv_freq=inv_freq, k=k, q_out=q_out, k_out=k_out)
-    batch, rows, heads, dh = q.shape
-    pairs = [int(n) for n in pairs]
-    if not 1 <= len(pairs) <= IM_MAX_AXES:
-        raise ValueError(f"{what}: 1 to {IM_MAX_AXES} axes, got {len(pairs)}")
+    dt, shape = q.dtype, q.shape
+    batch, rows, heads, dh = shape
+    if q_out is None:
+        q_out = torch.empty(shape, dtype=dt, device=q.device)
+    axes = len(pairs)
+    if not 1 <= axes <= IM_MAX_AXES:
+        raise ValueError(f"{what}: 1 to {IM_MAX_AXES} axes, got {axes}")
+    _needed(what, "pos", pos)
+    _needed(what, "inv_freq", inv_freq)
     shared = pos.dim() == 2
-    _want(what, "pos", pos, (rows, len(pairs)) if shared else (batch, rows, len(pairs)), torch.float32)
-    _want(what, "inv_freq", inv_freq, (sum(pairs),), torch.float32)
-    s = ImRotary(batch, rows, len(pairs), (C.c_int32 * IM_MAX_AXES)(*pairs), heads, 0 if k is None else k.shape[2], dh, bool(interleaved),
-                 bool(inverse), _dtype(q.dtype))
-    views = [_view(what, "q", q, q.shape, q.dtype), _view(what, "q_out", q_out, q.shape, q.dtype)]
+    kh = 0 if k is None else k.shape[2]
+    s = ImRotary(batch, rows, axes, (C.c_int32 * IM_MAX_AXES)(*pairs), heads, kh, dh, bool(interleaved), bool(inverse), _dtype(dt))
+    vk = vk_out = None
     if k is not None:
-        shape = torch.Size((batch, rows, k.shape[2], dh))
-        views += [_view(what, "k", k, shape, q.dtype), _view(what, "k_out", k_out, shape, q.dtype)]
-    else:
-        views += [None, None]
-    _check(lib().im_rotary_apply(C.byref(s), _p(pos), 0 if shared else rows * len(pairs), _p(inv_freq), *views, _stream()))
+        kshape = (batch, rows, kh, dh)
+        if k_out is None:
+            k_out = torch.empty(kshape, dtype=dt, device=q.device)
+        vk, vk_out = _view(what, "k", k, kshape, dt, dev), _view(what, "k_out", k_out, kshape, dt, dev)
+    f32 = torch.float32
+    _check((_lib or lib()).im_rotary_apply(s, _want(what, "pos", pos, (rows, axes) if shared else (batch, rows, axes), f32, dev),
+                                           0 if shared else rows * axes, _want(what, "inv_freq", inv_freq, (sum(pairs),), f32, dev),
+                                           _view(what, "q", q, shape, dt, dev), _view(what, "q_out", q_out, shape, dt, dev), vk, vk_out, _raw_stream(dev)))
     return q_out, k_out
 
 
@@ -478,23 +505,20 @@ def im_core_attention_sizes(core):
     return a.value, f.value, b.value
 
 
-def _core_rules(what, core, shapes, rules):
-    """im_core_rules_t of the arrays that are given, their shapes checked."""
-    batch, tq, tk = shapes
-    want = {"valid_len": ((batch, core.n_seg), torch.int32), "key_pad": ((batch, tk), torch.uint8), "q_pos": ((batch, tq), torch.float32),
-            "k_pos": ((batch, tk), torch.float32), "slope": ((core.n_heads,), torch.float32), "prefix": ((batch,), torch.float32),
-            "q_doc": ((batch, tq), torch.int32), "k_doc": ((batch, tk), torch.int32)}
-    r = ImCoreRules()
-    for name, t in rules.items():
-        if t is not None:
-            _want(what, name, t, *want[name])
-            setattr(r, name, t.data_ptr())
-    return r
-
-
 def _core_shapes(core):
-    tq, tk = sum(core.q_len[:core.n_seg]), sum(core.k_len[:core.n_seg])
-    return torch.Size((core.batch, tq, core.n_heads, core.head_dim)), torch.Size((core.batch, tk, core.n_kv_heads, core.head_dim)), (core.batch, tq, tk)
+    """(batch, query rows, key rows, heads, bytes of `saved`)"""
+    n = core.n_seg
+    tq, tk = sum(core.q_len[:n]), sum(core.k_len[:n])
+    rows = core.batch * core.n_heads * tq * 4
+    return core.batch, tq, tk, core.n_heads, (rows * core.head_dim + 255 & ~255) + (rows + 255 & ~255)
+
+
+def _core_rules(what, core, batch, tq, tk, dev, valid_len, key_pad, q_pos, k_pos, slope, prefix, q_doc, k_doc):
+    i32, f32 = torch.int32, torch.float32
+    return ImCoreRules(_want(what, "valid_len", valid_len, (batch, core.n_seg), i32, dev), _want(what, "key_pad", key_pad, (batch, tk), torch.uint8, dev),
+                       _want(what, "q_pos", q_pos, (batch, tq), f32, dev), _want(what, "k_pos", k_pos, (batch, tk), f32, dev),
+                       _want(what, "slope", slope, (core.n_heads,), f32, dev), _want(what, "prefix", prefix, (batch,), f32, dev),
+                       _want(what, "q_doc", q_doc, (batch, tq), i32, dev), _want(what, "k_doc", k_doc, (batch, tk), i32, dev))
 
 
 def im_core_attention_fwd(core, q, k, v, valid_len=None, key_pad=None, q_pos=None, k_pos=None, slope=None, prefix=None, q_doc=None,
@@ -503,20 +527,18 @@ def im_core_attention_fwd(core, q, k, v, valid_len=None, key_pad=None, q_pos=Non
     given; see include/imattn.h.  lse: fp32 [B, heads, Tq] or None; saved / workspace: uint8 buffers of
     im_core_attention_sizes (saved None for inference)."""
     what = "im_core_attention_fwd"
+    dev = _device(what, q)
     if o is None:
         o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    rules = dict(valid_len=valid_len, key_pad=key_pad, q_pos=q_pos, k_pos=k_pos, slope=slope, prefix=prefix, q_doc=q_doc, k_doc=k_doc)
-    _on_device(q.device, what, k=k, v=v, o=o, lse=lse, saved=saved, workspace=workspace, **rules)
-    shape_q, shape_k, n = _core_shapes(core)
-    r = _core_rules(what, core, n, rules)
-    dt = torch.bfloat16 if core.dtype == IM_DTYPE_BF16 else torch.float32
-    views = [_view(what, "q", q, shape_q, dt), _view(what, "k", k, shape_k, dt), _view(what, "v", v, shape_k, dt), _view(what, "o", o, shape_q, dt)]
-    _want(what, "lse", lse, (core.batch, core.n_heads, n[1]), torch.float32, True)
-    keep, have = _want_bytes(what, "saved", saved)
-    if saved is not None and have < im_core_attention_sizes(core)[0]:
-        raise ValueError(f"{what}: saved has {have} bytes, {im_core_attention_sizes(core)[0]} are needed")
-    ws, nbytes = _want_bytes(what, "workspace", workspace)
-    _check(lib().im_core_attention_fwd(C.byref(core), C.byref(r), *views, _p(lse), keep, ws, nbytes, _stream()))
+    batch, tq, tk, heads, need = _core_shapes(core)
+    dt = _TORCH_TYPES[core.dtype == IM_DTYPE_BF16]
+    shape_q, shape_k = (batch, tq, heads, core.head_dim), (batch, tk, core.n_kv_heads, core.head_dim)
+    r = _core_rules(what, core, batch, tq, tk, dev, valid_len, key_pad, q_pos, k_pos, slope, prefix, q_doc, k_doc)
+    keep, _ = _bytes(what, "saved", saved, dev, need)
+    ws, nbytes = _bytes(what, "workspace", workspace, dev)
+    _check((_lib or lib()).im_core_attention_fwd(core, r, _view(what, "q", q, shape_q, dt, dev), _view(what, "k", k, shape_k, dt, dev),
+                                                 _view(what, "v", v, shape_k, dt, dev), _view(what, "o", o, shape_q, dt, dev),
+                                                 _want(what, "lse", lse, (batch, heads, tq), torch.float32, dev), keep, ws, nbytes, _raw_stream(dev)))
     return o
 
 
@@ -525,19 +547,18 @@ def im_core_attention_bwd(core, q, k, v, saved, d_o, dq, dk, dv, dslope=None, va
     """Gradients of im_core_attention_fwd with the same arguments and its `saved`: dq, dk, dv and, if given, dslope (fp32
     [heads]) are overwritten."""
     what = "im_core_attention_bwd"
-    rules = dict(valid_len=valid_len, key_pad=key_pad, q_pos=q_pos, k_pos=k_pos, slope=slope, prefix=prefix, q_doc=q_doc, k_doc=k_doc)
-    _on_device(q.device, what, k=k, v=v, saved=saved, d_o=d_o, dq=dq, dk=dk, dv=dv, dslope=dslope, workspace=workspace, **rules)
-    shape_q, shape_k, n = _core_shapes(core)
-    r = _core_rules(what, core, n, rules)
-    dt = torch.bfloat16 if core.dtype == IM_DTYPE_BF16 else torch.float32
-    views = [_view(what, m, t, shape_q if m in ("q", "d_o", "dq") else shape_k, dt)
-             for m, t in (("q", q), ("k", k), ("v", v), ("d_o", d_o), ("dq", dq), ("dk", dk), ("dv", dv))]
-    _want(what, "dslope", dslope, (core.n_heads,), torch.float32, True)
-    keep, have = _want_bytes(what, "saved", saved)
-    if saved is not None and have < im_core_attention_sizes(core)[0]:
-        raise ValueError(f"{what}: saved has {have} bytes, {im_core_attention_sizes(core)[0]} are needed")
-    ws, nbytes = _want_bytes(what, "workspace", workspace)
-    _check(lib().im_core_attention_bwd(C.byref(core), C.byref(r), *views[:3], keep, *views[3:], _p(dslope), ws, nbytes, _stream()))
+    dev = _device(what, q)
+    batch, tq, tk, heads, need = _core_shapes(core)
+    dt = _TORCH_TYPES[core.dtype == IM_DTYPE_BF16]
+    shape_q, shape_k = (batch, tq, heads, core.head_dim), (batch, tk, core.n_kv_heads, core.head_dim)
+    r = _core_rules(what, core, batch, tq, tk, dev, valid_len, key_pad, q_pos, k_pos, slope, prefix, q_doc, k_doc)
+    keep, _ = _bytes(what, "saved", saved, dev, need)
+    ws, nbytes = _bytes(what, "workspace", workspace, dev)
+    _check((_lib or lib()).im_core_attention_bwd(core, r, _view(what, "q", q, shape_q, dt, dev), _view(what, "k", k, shape_k, dt, dev),
+                                                 _view(what, "v", v, shape_k, dt, dev), keep, _view(what, "d_o", d_o, shape_q, dt, dev),
+                                                 _view(what, "dq", dq, shape_q, dt, dev), _view(what, "dk", dk, shape_k, dt, dev),
+                                                 _view(what, "dv", dv, shape_k, dt, dev), _want(what, "dslope", dslope, (heads,), torch.float32, dev), ws,
+                                                 nbytes, _raw_stream(dev)))
     return dq, dk, dv
 
 

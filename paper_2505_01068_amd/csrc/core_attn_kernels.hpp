@@ -417,6 +417,11 @@ struct CoreLds {
   Range own[CORE_WAVES];
 };
 
+// A value that the compiler takes for new here: what is made of it is made here, not kept in registers from before the loop.
+__device__ __forceinline__ int late(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
 template <bool FEW>
 __device__ __forceinline__ void team_sync() {
   if constexpr (FEW) {   // one wave: its LDS instructions stay in order, only the compiler must not move them
@@ -493,17 +498,27 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>
   const int b = at.b, dh = a.dh;
 
   // ---- the owned row of this lane ----
-  const int col = at.own0 + (FEW ? 0 : 32 * wave) + (lane & 31);
-  const bool in_range = col < at.own_n;
-  unsigned own_t = (unsigned)col, own_g = 0;
-  if (!OWN_KEYS && a.G > 1) udivmod((unsigned)col, (unsigned)a.G, own_t, own_g);
-  const int own_row = (OWN_KEYS ? a.k_off[at.seg] : a.q_off[at.seg]) + (int)own_t;
-  const int own_head = OWN_KEYS ? at.kvh : at.kvh * a.G + (int)own_g;
+  struct OwnRow { int t, row, head; long stat; bool is; };   // position in its segment, in the tensor; head; place among the statistics of query rows
+  auto own_place = [&](int l) {
+    const int col = at.own0 + (FEW ? 0 : 32 * wave) + (l & 31);
+    unsigned t = (unsigned)col, g = 0;
+    if (!OWN_KEYS && a.G > 1) udivmod((unsigned)col, (unsigned)a.G, t, g);
+    OwnRow o;
+    o.is = col < at.own_n;
+    o.t = (int)t;
+    o.row = (OWN_KEYS ? a.k_off[at.seg] : a.q_off[at.seg]) + (int)t;
+    o.head = OWN_KEYS ? at.kvh : at.kvh * a.G + (int)g;
+    o.stat = ((long)b * a.H + o.head) * a.Tq + o.row;
+    return o;
+  };
+  const OwnRow me = own_place(lane);
+  const bool in_range = me.is;
+  const int own_row = me.row, own_head = me.head;
+  const long own_stat = me.stat;
   bool own_valid = in_range;
-  if (OWN_KEYS && a.valid_len) own_valid = in_range && (int)own_t < a.valid_len[b * a.n_seg + at.seg];
+  if (OWN_KEYS && a.valid_len) own_valid = in_range && me.t < a.valid_len[b * a.n_seg + at.seg];
   const float prefix = a.prefix ? a.prefix[b] : IM_NEG_INF;
   const RowInfo own = OWN_KEYS ? key_info(a, prefix, key_raw(a, b, own_row, own_valid)) : query_info(a, query_raw(a, b, own_row, own_valid));
-  const long own_stat = ((long)b * a.H + own_head) * a.Tq + own_row;   // of a query row
 
   Frag own1[2 * ND], own2[BWD ? 2 * ND : 1];   // Q (and dO), or K and V
   if constexpr (!OWN_KEYS) {
@@ -604,22 +619,23 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>
       for (int i = 0; i < C::N; ++i) {
         unsigned o = off[i];
         if (n < ROWS) {
-          const int u = tt + i * C::TEAM;
+          const int u = late(tt) + i * C::TEAM;
           o = (unsigned)(min(TL::row_of(u), n - 1) * view.row * (long)sizeof(T)) + 16 * TL::unit_of(u);
         }
         if (has[i]) copy16(from, o, to + (i * C::TEAM + (FEW ? 0 : wave * 64)) * 16);
       }
     } else if (words) {   // 4 bytes a lane
+      const int t0 = late(tt);
 #pragma unroll(C::N > 2 ? 2 : 4)
       for (int i = 0; i < 4 * C::N; ++i) {
-        const int w = tt + i * C::TEAM, at = 16 * TL::unit_of(w >> 2) + 4 * (w & 3);
+        const int w = t0 + i * C::TEAM, at = 16 * TL::unit_of(w >> 2) + 4 * (w & 3);
         const unsigned o = (unsigned)min(TL::row_of(w >> 2), n - 1) * (unsigned)(view.row * (long)sizeof(T)) + at;
         if (at < dh * (int)sizeof(T)) copy4(from, o, to + (i * C::TEAM + (FEW ? 0 : wave * 64)) * 4);
       }
     } else {   // element by element, through registers
 #pragma unroll 1
       for (int i = 0; i < C::N; ++i) {
-        const int u = tt + i * C::TEAM;
+        const int u = late(tt) + i * C::TEAM;
         *(u32x4*)(to + u * 16) = load_unit(from + min(TL::row_of(u), n - 1) * view.row, TL::unit_of(u) * EPC, dh, false);
       }
     }
@@ -660,11 +676,12 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>
   // values of a tile with masked pairs that are not finite: 0 in their place, and a mark on their row
   auto clean = [&](int buf) {
     u32x4* units = (u32x4*)team.tile[buf];
+    const int t0 = late(tt);
     unsigned bits = 0;
 #pragma unroll
     for (int i = 0; i < 2 * C::N; ++i) {
-      const int u = tt + i * C::TEAM;
-      if (TL::unit_of(u % TL::SLOTS) * EPC >= 32 * ND) continue;   // half a panel that nothing reads or writes (ND = 1)
+      const int u = t0 + i * C::TEAM;
+      if (TL::BF && ND == 1 && TL::unit_of(u % TL::SLOTS) >= 4) continue;   // half a panel that nothing reads or writes
       const u32x4 x = units[u];
 #pragma unroll
       for (int w = 0; w < 4; ++w) bits |= odd_bits(T(), x[w]);
@@ -672,8 +689,8 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>
     if (!odd(T(), bits)) return;
 #pragma unroll 1
     for (int i = 0; i < 2 * C::N; ++i) {
-      const int u = tt + i * C::TEAM;
-      if (TL::unit_of(u % TL::SLOTS) * EPC >= 32 * ND) continue;
+      const int u = t0 + i * C::TEAM;
+      if (TL::BF && ND == 1 && TL::unit_of(u % TL::SLOTS) >= 4) continue;
       u32x4 x = units[u];
       bits = 0;
 #pragma unroll
@@ -894,32 +911,38 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>
       return make_int4(__builtin_amdgcn_readfirstlane(e.x), __builtin_amdgcn_readfirstlane(e.y), __builtin_amdgcn_readfirstlane(e.z),
                        OWN_KEYS ? __builtin_amdgcn_readfirstlane(e.w) : 0);
     };
-    int4 e = next();
-    int buf = 0;
-    if (BUFS == 2 && e.y) fetch(e, 0);
-    while (e.y) {
-      const bool part = e.z == TILE_PART;
-      if (BUFS == 1) fetch(e, 0);
+    // Tile e is at hand, its copies were asked for one turn ago; those of the tile ahead go into the other buffer meanwhile.  (With one
+    // buffer a tile's copies are waited for.)  The first turn only asks for copies.
+    int4 e = make_int4(0, 0, 0, 0);
+    int buf = BUFS - 1;
+    for (;;) {
       const int4 ahead = next();
-      arrive(buf, part, e.y);
-      team_sync<FEW>();   // all waves' copies are there, and nobody reads the other buffer any more
-      ++stamp;
+      if (e.y) {
+        arrive(buf, e.z == TILE_PART, e.y);
+        team_sync<FEW>();   // all waves' copies are there, and nobody reads the other buffer any more
+      }
       if (BUFS == 2 && ahead.y) fetch(ahead, buf ^ 1);
-      if (part) {
-        clean(buf);
-        team_sync<FEW>();
-      }
-      if constexpr (BIAS && OWN_KEYS) {
-        typedef const float __attribute__((address_space(4))) * const_ptr;   // (a scalar load: no wait for the copies in flight)
-        tile_slope2 = ((const_ptr)(uintptr_t)a.slope)[head0 + e.w] * LOG2E;
-      }
+      if (e.y) {
+        const bool part = e.z == TILE_PART;
+        ++stamp;
+        if (part) {
+          clean(buf);
+          team_sync<FEW>();
+        }
+        if constexpr (BIAS && OWN_KEYS) {
+          typedef const float __attribute__((address_space(4))) * const_ptr;   // (a scalar load: no wait for the copies in flight)
+          tile_slope2 = ((const_ptr)(uintptr_t)a.slope)[head0 + e.w] * LOG2E;
+        }
 #pragma unroll
-      for (int r = 0; r < ROWS / 32; ++r) {
-        f32x16 sc, dp;
-        products(buf, 32 * r, sc, dp);
-        block(buf, 32 * r, part, sc, dp);
+        for (int r = 0; r < ROWS / 32; ++r) {
+          f32x16 sc, dp;
+          products(buf, 32 * r, sc, dp);
+          block(buf, 32 * r, part, sc, dp);
+        }
+        if constexpr (FEW) team_sync<FEW>();
       }
-      if constexpr (FEW) team_sync<FEW>();
+      if (!ahead.y) break;
+      if (BUFS == 1) fetch(ahead, 0);
       buf ^= BUFS - 1;
       e = ahead;
     }
@@ -1000,27 +1023,28 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>
     }
     if (wave != 0) return;
   }
-  if (!in_range) return;
+  const OwnRow to = own_place(late(lane));   // made again rather than kept
+  if (!to.is) return;
   if constexpr (WHICH == CORE_FWD) {
     if (a.splits > 1) {
-      const long row = ((long)at.split * a.B * a.H + (long)b * a.H + own_head) * a.Tq + own_row;
+      const long row = ((long)at.split * a.B * a.H * a.Tq) + to.stat;
       store_row<float, ND>(a.part_o + row * dh, dh, dh % 4 == 0, h, acc1, 1.f);
       if (h == 0) { a.part_ml[2 * row] = m; a.part_ml[2 * row + 1] = l; }
       return;
     }
     const float inv = l == 0.f ? 0.f : 1.f / l, lse2 = l == 0.f ? IM_NEG_INF : m + log2f(l);
-    store_row<T, ND>(head_of<T>(a.o, b, own_row, own_head), dh, a.vec & VEC_O, h, acc1, inv);
-    if (a.o32) store_row<float, ND>(a.o32 + own_stat * dh, dh, dh % 4 == 0, h, acc1, inv);
+    store_row<T, ND>(head_of<T>(a.o, b, to.row, to.head), dh, a.vec & VEC_O, h, acc1, inv);
+    if (a.o32) store_row<float, ND>(a.o32 + to.stat * dh, dh, dh % 4 == 0, h, acc1, inv);
     if (h == 0) {
-      if (a.lse) a.lse[own_stat] = lse2 * LN2;
-      if (a.lse2) a.lse2[own_stat] = lse2;
+      if (a.lse) a.lse[to.stat] = lse2 * LN2;
+      if (a.lse2) a.lse2[to.stat] = lse2;
     }
   } else if constexpr (WHICH == CORE_DQ) {
-    store_row<T, ND>(head_of<T>(a.dq, b, own_row, own_head), dh, a.vec & VEC_DQ, h, acc1, a.scale);
-    if (BIAS && a.dslope_rows && h == 0) a.dslope_rows[own_stat] = dslope + rest * mean_gap;
+    store_row<T, ND>(head_of<T>(a.dq, b, to.row, to.head), dh, a.vec & VEC_DQ, h, acc1, a.scale);
+    if (BIAS && a.dslope_rows && h == 0) a.dslope_rows[to.stat] = dslope + rest * mean_gap;
   } else {
-    store_row<T, ND>(head_of<T>(a.dk, b, own_row, own_head), dh, a.vec & VEC_DK, h, acc1, a.scale);
-    store_row<T, ND>(head_of<T>(a.dv, b, own_row, own_head), dh, a.vec & VEC_DV, h, acc2, 1.f);
+    store_row<T, ND>(head_of<T>(a.dk, b, to.row, to.head), dh, a.vec & VEC_DK, h, acc1, a.scale);
+    store_row<T, ND>(head_of<T>(a.dv, b, to.row, to.head), dh, a.vec & VEC_DV, h, acc2, 1.f);
   }
 }
 
