@@ -335,7 +335,7 @@ def _dtype(t):
 def _device(what, x):
     """The call goes to the current device's current stream: every tensor has to live on that device.  Its index."""
     i = x.get_device()
-    if i < 0 or i != torch.cuda.current_device():
+    if i < 0 or i != torch._C._cuda_getDevice():
         raise ValueError(f"{what}: tensors must be on the current GPU, got {x.device}")
     return i
 

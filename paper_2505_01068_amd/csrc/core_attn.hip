@@ -65,48 +65,63 @@ struct CoreLaunch {
   unsigned grid;
 };
 
-static long seg_tiles(int n, int own) { return ((long)n + own - 1) / own; }
+static long row_tiles(long n, int own) { return (n + own - 1) / own; }
 
-// Shape of a launch that owns query rows (or key rows), and the owned segments in launch order.
-// few: four waves to 32 rows instead of 128 -- where 128 rows a workgroup would leave CUs idle or half of the rows empty.
-// splits (forward with few): until 4 workgroups a CU, each with at least 16 tiles of 32 keys.
-static CoreLaunch core_launch(const im_core_t* s, bool own_keys, bool may_split, CoreArgs* a) {
+// Shape of a launch that owns query rows (or key rows), and its groups of rows (written to *a if given).
+// Neighbouring segments with the same live partners are one group -- three segments of one new token each are one tile, not three that read the
+// cache three times -- unless per-sample lengths cut their ends off, or a tile across the border of two owned segments would mix the times or
+// documents by which streamed tiles are skipped (`sparse`; one tile that holds both whole is still better than two).
+// few: four waves to 32 rows instead of 128, where 128 rows a workgroup would leave CUs idle or half of the rows empty.
+// splits (forward with few): two workgroups a CU, all at once, each with at least 16 tiles of 32 keys.  (16 requests against 17408 keys:
+// 59 us; with four workgroups a CU, in two turns, 69 us.)
+static CoreLaunch core_launch(const im_core_t* s, bool own_keys, bool may_split, bool lengths, bool sparse, CoreArgs* a) {
   CoreLaunch L = {};
   const int G = own_keys ? 1 : s->n_heads / s->n_kv_heads;
   const int32_t* own_len = own_keys ? s->k_len : s->q_len;
-  const int32_t* other_len = own_keys ? s->q_len : s->k_len;
+  const int32_t* str_len = own_keys ? s->q_len : s->k_len;
+  auto live = [&](int own, int str) { return str_len[str] > 0 && ((s->live_mask >> (own_keys ? str * s->n_seg + own : own * s->n_seg + str)) & 1ull); };
+  struct Group { int row0, len, seg; unsigned live; long work; } own[IM_MAX_SEG], str[IM_MAX_SEG];
+  int n_own = 0, n_str = 0;
+  // streamed groups: neighbours that every owned segment sees or does not see together
+  for (int j = 0, row = 0; j < s->n_seg; row += str_len[j++]) {
+    if (str_len[j] == 0) continue;
+    bool alike = n_str > 0 && !(lengths && !own_keys);
+    for (int i = 0; i < s->n_seg && alike; ++i) alike = own_len[i] == 0 || live(i, j) == live(i, str[n_str - 1].seg);
+    if (alike) str[n_str - 1].len += str_len[j];
+    else str[n_str++] = {row, str_len[j], j, 0u, 0};
+  }
+  for (int i = 0, row = 0; i < s->n_seg; row += own_len[i++]) {
+    if (own_len[i] == 0) continue;
+    Group g = {row, own_len[i], i, 0u, 0};
+    for (int j = 0; j < n_str; ++j)
+      if (live(i, str[j].seg)) { g.live |= 1u << j; g.work += str[j].len; }
+    if (n_own > 0 && own[n_own - 1].live == g.live && !(lengths && own_keys) && (!sparse || ((long)own[n_own - 1].len + g.len) * G <= 32)) own[n_own - 1].len += g.len;
+    else own[n_own++] = g;
+  }
   const long groups = (long)s->batch * s->n_kv_heads;
   long t128 = 0, t32 = 0, most = 0;
-  long work[IM_MAX_SEG];
-  for (int i = 0; i < s->n_seg; ++i) {
-    t128 += seg_tiles(own_len[i] * G, 128);
-    t32 += seg_tiles(own_len[i] * G, 32);
-    work[i] = 0;
-    for (int j = 0; j < s->n_seg; ++j) {
-      const int bit = own_keys ? j * s->n_seg + i : i * s->n_seg + j;
-      if ((s->live_mask >> bit) & 1ull) work[i] += other_len[j];
-    }
-    most = std::max(most, work[i]);
+  for (int i = 0; i < n_own; ++i) {
+    t128 += row_tiles((long)own[i].len * G, 128);
+    t32 += row_tiles((long)own[i].len * G, 32);
+    most = std::max(most, own[i].work);
   }
-#ifndef FEW_MULT
-#define FEW_MULT 1
-#endif
-  L.few = t128 * groups < FEW_MULT * cu_count() || 4 * t128 > 2 * t32;
-  const int own = L.few ? 32 : 128;
+  L.few = t128 * groups < cu_count() || 4 * t128 > 2 * t32;
   L.tiles = (int)(L.few ? t32 : t128);
   L.splits = 1;
-  if (may_split && L.few && L.tiles > 0) {
-    const long wgs = L.tiles * groups;
-    L.splits = (int)std::max<long>(1, std::min<long>((4l * cu_count() + wgs - 1) / wgs, most / (16 * 32)));
-  }
+  if (may_split && L.few && L.tiles > 0)
+    L.splits = (int)std::max<long>(1, std::min<long>(2l * cu_count() / (L.tiles * groups), most / (16 * 32)));
   const long grid = (long)L.tiles * groups * L.splits;
   L.grid = grid < (1l << 24) ? (unsigned)grid : 0xffffffffu;
   if (a) {
-    int n = s->n_seg;
-    for (int i = 0; i < n; ++i) a->order[i] = i;
-    std::stable_sort(a->order, a->order + n, [&](int x, int y) { return work[x] > work[y]; });
+    std::stable_sort(own, own + n_own, [](const Group& x, const Group& y) { return x.work > y.work; });
+    a->own_groups = n_own;
+    a->str_groups = n_str;
     a->tile_prefix[0] = 0;
-    for (int k = 0; k < n; ++k) a->tile_prefix[k + 1] = a->tile_prefix[k] + (int)seg_tiles(own_len[a->order[k]] * G, own);
+    for (int i = 0; i < n_own; ++i) {
+      a->own_row0[i] = own[i].row0; a->own_len[i] = own[i].len; a->own_seg[i] = own[i].seg; a->own_live[i] = own[i].live;
+      a->tile_prefix[i + 1] = a->tile_prefix[i] + (int)row_tiles((long)own[i].len * G, L.few ? 32 : 128);
+    }
+    for (int j = 0; j < n_str; ++j) { a->str_row0[j] = str[j].row0; a->str_len[j] = str[j].len; a->str_seg[j] = str[j].seg; }
     a->splits = L.splits;
   }
   return L;
@@ -134,7 +149,7 @@ static int core_check(const char* what, const im_core_t* s) {
   if (!(s->scale >= 0.f) || isinf(s->scale)) return refuse(IM_ERR_INVALID, "%s: scale must be finite and >= 0", what);
   if (s->cap != 0.f && !(s->cap >= 0.01f && s->cap <= 1000.f)) return refuse(IM_ERR_INVALID, "%s: cap must be 0 or in 0.01..1000", what);
   for (int own_keys = 0; own_keys < 2; ++own_keys)
-    if (core_launch(s, own_keys, !own_keys, nullptr).grid == 0xffffffffu)
+    if (core_launch(s, own_keys, !own_keys, true, true, nullptr).grid == 0xffffffffu)
       return refuse(IM_ERR_INVALID, "%s: problem too large (2^24 workgroups or more)", what);
   return IM_OK;
 }
@@ -157,13 +172,7 @@ static int core_rules(const char* what, const im_core_t* s, const im_core_rules_
 static void core_args(const im_core_t* s, const im_core_rules_t* r, CoreArgs* a) {
   memset(a, 0, sizeof(*a));
   a->B = s->batch; a->H = s->n_heads; a->Hkv = s->n_kv_heads; a->G = s->n_heads / s->n_kv_heads; a->dh = s->head_dim; a->n_seg = s->n_seg;
-  for (int i = 0; i < s->n_seg; ++i) {
-    a->q_off[i + 1] = a->q_off[i] + s->q_len[i];
-    a->k_off[i + 1] = a->k_off[i] + s->k_len[i];
-    for (int j = 0; j < s->n_seg; ++j)
-      if ((s->live_mask >> (i * s->n_seg + j)) & 1ull) { a->q_live[i] |= 1u << j; a->k_live[j] |= 1u << i; }
-  }
-  a->Tq = a->q_off[s->n_seg]; a->Tk = a->k_off[s->n_seg];
+  for (int i = 0; i < s->n_seg; ++i) { a->Tq += s->q_len[i]; a->Tk += s->k_len[i]; }
   a->causal = s->causal != 0;
   a->cap = s->cap;
   if (s->scale == 0.f) a->cap = 0.f;   // every score is 0, capped or not
@@ -204,7 +213,8 @@ static CoreSizes core_sizes(const im_core_t* s) {
   CoreSizes z;
   z.o32 = round256(rows * s->head_dim * 4);
   z.saved = z.o32 + round256(rows * 4);
-  const int splits = core_launch(s, false, true, nullptr).splits;
+  // (documents are not known here: enough for either way of grouping)
+  const int splits = std::max(core_launch(s, false, true, false, false, nullptr).splits, core_launch(s, false, true, false, true, nullptr).splits);
   z.part_o = splits > 1 ? round256(splits * rows * s->head_dim * 4) : 0;
   z.fwd = splits > 1 ? z.part_o + round256(splits * rows * 8) : 0;
   z.stat = round256(rows * 4);
@@ -257,7 +267,7 @@ int im_core_attention_fwd(const im_core_t* shape, const im_core_rules_t* rules, 
   core_units(&a, es);
   if (saved) { a.o32 = (float*)saved; a.lse2 = (float*)((char*)saved + z.o32); }
   a.part_o = (float*)workspace; a.part_ml = (float*)((char*)workspace + z.part_o);
-  const CoreLaunch L = core_launch(shape, false, true, &a);
+  const CoreLaunch L = core_launch(shape, false, true, a.valid_len != nullptr, a.causal || a.q_doc, &a);
   if (!L.grid) return IM_OK;
   hipStream_t st = (hipStream_t)hip_stream;
   ProfScope ps(PF_ATTN_FWD, st);
@@ -301,13 +311,13 @@ int im_core_attention_bwd(const im_core_t* shape, const im_core_rules_t* rules, 
   a.delta = (float*)workspace;
   a.dslope_rows = dslope ? (float*)((char*)workspace + z.stat) : nullptr;
   hipStream_t st = (hipStream_t)hip_stream;
-  const CoreLaunch Lq = core_launch(shape, false, false, &a);
+  const CoreLaunch Lq = core_launch(shape, false, false, a.valid_len != nullptr, a.causal || a.q_doc, &a);
   if (Lq.grid) {
     ProfScope ps(PF_ATTN_DQ, st);
     (bf ? launch_core_dq_bf16 : launch_core_dq_f32)(Lq.few, a, Lq.grid, st);
   }
   if (dslope) hipLaunchKernelGGL(core_dslope_kernel, dim3(a.H), dim3(1024), 0, st, a.dslope_rows, a.B, a.H, a.Tq, dslope);
-  const CoreLaunch Lk = core_launch(shape, true, false, &a);
+  const CoreLaunch Lk = core_launch(shape, true, false, a.valid_len != nullptr, a.causal || a.q_doc, &a);
   if (Lk.grid) {
     ProfScope ps(PF_ATTN_DKV, st);
     (bf ? launch_core_dkv_bf16 : launch_core_dkv_f32)(Lk.few, a, Lk.grid, st);

@@ -8,10 +8,12 @@ namespace imattn {
 // row t * G + g of a segment, so that the heads that share a key head share its tiles.
 struct CoreArgs {
   int B, H, Hkv, G, dh, n_seg, Tq, Tk;
-  int q_off[IM_MAX_SEG + 1], k_off[IM_MAX_SEG + 1];
-  unsigned q_live[IM_MAX_SEG], k_live[IM_MAX_SEG];   // query segment -> live key segments, and back
-  // tiles of the kernel's own rows: segments in launch order, those with most to read first
-  int order[IM_MAX_SEG], tile_prefix[IM_MAX_SEG + 1];
+  // The launch's owned rows (queries; keys for dK/dV) and streamed rows in groups of neighbouring segments that the pattern of live blocks
+  // treats alike.  Owned groups in launch order, those with most to read first; tile_prefix counts their tiles.  seg: the group's
+  // (only) segment, where valid_len needs one.
+  int own_groups, own_row0[IM_MAX_SEG], own_len[IM_MAX_SEG], own_seg[IM_MAX_SEG], tile_prefix[IM_MAX_SEG + 1];
+  unsigned own_live[IM_MAX_SEG];   // bit per streamed group
+  int str_groups, str_row0[IM_MAX_SEG], str_len[IM_MAX_SEG], str_seg[IM_MAX_SEG];
   int splits;                     // workgroups that share the keys of one tile (forward)
   unsigned vec, words;            // bit per tensor (VecBit): heads in aligned units of 16 bytes, of 4 bytes
   int causal;

@@ -413,7 +413,7 @@ template <class T, int ND, bool FEW, CoreKernel WHICH>
 struct CoreLds {
   static constexpr int TEAMS = FEW ? CORE_WAVES : 1;
   __align__(16) TeamLds<T, ND, FEW, WHICH> team[TEAMS];
-  int4 list[CORE_LIST];       // first row, rows, class, head of the group (dK/dV)
+  int4 list[CORE_LIST];       // first row, rows, class | waves that skip it << 8 | waves that see all of it << 12, head of the group (dK/dV)
   Range own[CORE_WAVES];
 };
 
@@ -443,27 +443,27 @@ __device__ __forceinline__ unsigned clean_bits(bf16_t, unsigned u) {
 }
 __device__ __forceinline__ unsigned clean_bits(float, unsigned u) { return (u & 0x7f800000u) == 0x7f800000u ? 0u : u; }
 
-// Where a workgroup stands: batch element, key head, owned segment, first owned row, split.
-struct Place { int b, kvh, seg, own0, own_n, split; };
+// Where a workgroup stands: batch element, key head, owned group, first owned row in it, the group's rows, split.
+struct Place { int b, kvh, group, own0, own_n, split; };
 
 template <bool OWN_KEYS, int OWN>
-__device__ __forceinline__ Place place_of(const CoreArgs& a, int nord) {
+__device__ __forceinline__ Place place_of(const CoreArgs& a) {
   int bx, by, bz;
   xcd_block_index(bx, by, bz);   // 1-d grid
-  const int tiles = a.tile_prefix[nord];
+  const int tiles = a.tile_prefix[a.own_groups];
   unsigned rest, tile, bh, split, b, kvh;
   udivmod((unsigned)bx, (unsigned)tiles, rest, tile);
   udivmod(rest, (unsigned)a.splits, bh, split);
   udivmod(bh, (unsigned)a.Hkv, b, kvh);
   int k = 0;
-  while (k + 1 < nord && (int)tile >= a.tile_prefix[k + 1]) ++k;
+  while (k + 1 < a.own_groups && (int)tile >= a.tile_prefix[k + 1]) ++k;
   Place p;
   p.b = __builtin_amdgcn_readfirstlane((int)b);
   p.kvh = __builtin_amdgcn_readfirstlane((int)kvh);
   p.split = __builtin_amdgcn_readfirstlane((int)split);
   k = __builtin_amdgcn_readfirstlane(k);
-  p.seg = a.order[k];
-  p.own_n = OWN_KEYS ? a.k_off[p.seg + 1] - a.k_off[p.seg] : (a.q_off[p.seg + 1] - a.q_off[p.seg]) * a.G;
+  p.group = k;
+  p.own_n = OWN_KEYS ? a.own_len[k] : a.own_len[k] * a.G;
   // the last tile of a segment first: under causality it sees most
   p.own0 = (a.tile_prefix[k + 1] - 1 - __builtin_amdgcn_readfirstlane((int)tile)) * OWN;
   return p;
@@ -494,11 +494,11 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), h = lane >> 5;
   const int tt = FEW ? lane : (int)threadIdx.x;     // thread of the team
   auto& team = lds.team[FEW ? wave : 0];
-  const Place at = place_of<OWN_KEYS, C::OWN>(a, a.n_seg);
+  const Place at = place_of<OWN_KEYS, C::OWN>(a);
   const int b = at.b, dh = a.dh;
 
   // ---- the owned row of this lane ----
-  struct OwnRow { int t, row, head; long stat; bool is; };   // position in its segment, in the tensor; head; place among the statistics of query rows
+  struct OwnRow { int t, row, head; long stat; bool is; };   // position in its group, in the tensor; head; place among the statistics of query rows
   auto own_place = [&](int l) {
     const int col = at.own0 + (FEW ? 0 : 32 * wave) + (l & 31);
     unsigned t = (unsigned)col, g = 0;
@@ -506,7 +506,7 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>
     OwnRow o;
     o.is = col < at.own_n;
     o.t = (int)t;
-    o.row = (OWN_KEYS ? a.k_off[at.seg] : a.q_off[at.seg]) + (int)t;
+    o.row = a.own_row0[at.group] + (int)t;
     o.head = OWN_KEYS ? at.kvh : at.kvh * a.G + (int)g;
     o.stat = ((long)b * a.H + o.head) * a.Tq + o.row;
     return o;
@@ -516,7 +516,7 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>
   const int own_row = me.row, own_head = me.head;
   const long own_stat = me.stat;
   bool own_valid = in_range;
-  if (OWN_KEYS && a.valid_len) own_valid = in_range && me.t < a.valid_len[b * a.n_seg + at.seg];
+  if (OWN_KEYS && a.valid_len) own_valid = in_range && me.t < a.valid_len[b * a.n_seg + a.own_seg[at.group]];
   const float prefix = a.prefix ? a.prefix[b] : IM_NEG_INF;
   const RowInfo own = OWN_KEYS ? key_info(a, prefix, key_raw(a, b, own_row, own_valid)) : query_info(a, query_raw(a, b, own_row, own_valid));
 
@@ -573,15 +573,14 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>
   const T *base_a = head_of<const T>(va, b, 0, head0), *base_b = head_of<const T>(vb, b, 0, head0);
   const bool vec_a = a.vec & (OWN_KEYS ? VEC_Q : VEC_K), vec_b = a.vec & (OWN_KEYS ? VEC_DO : VEC_V);
   const bool words_a = a.words & (OWN_KEYS ? VEC_Q : VEC_K), words_b = a.words & (OWN_KEYS ? VEC_DO : VEC_V);
-  const unsigned live = OWN_KEYS ? a.k_live[at.seg] : a.q_live[at.seg];
+  const unsigned live = a.own_live[at.group];
   const bool scan = a.causal || a.q_doc || (a.key_pad && !OWN_KEYS);   // classes that depend on the streamed rows' data
-  auto stream_len = [&](int j) {   // rows of streamed segment j that count
-    if (OWN_KEYS) return a.q_off[j + 1] - a.q_off[j];
-    const int n = a.k_off[j + 1] - a.k_off[j];
-    return a.valid_len ? min(n, max(a.valid_len[b * a.n_seg + j], 0)) : n;
+  auto stream_len = [&](int j) {   // rows of streamed group j that count
+    const int n = a.str_len[j];
+    return !OWN_KEYS && a.valid_len ? min(n, max(a.valid_len[b * a.n_seg + a.str_seg[j]], 0)) : n;
   };
   int total = 0;
-  for (int j = 0; j < a.n_seg; ++j)
+  for (int j = 0; j < a.str_groups; ++j)
     if ((live >> j) & 1u) total += (stream_len(j) + ROWS - 1) / ROWS * (OWN_KEYS ? a.G : 1);
   if (!mine.any) total = 0;
   const int first = (int)((long)total * at.split / a.splits), last = (int)((long)total * (at.split + 1) / a.splits);
@@ -719,7 +718,7 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>
         if (sizeof(T) == 2 || 16 * st < dh) dp = at_lane.rows(tb, row32, st, own2[st], dp, dh - 16 * st);
     }
   };
-  auto block = [&](int buf, int row32, bool part, const f32x16& sc, const f32x16& dp) {
+  auto block = [&](int buf, int row32, bool part, bool odd_values, const f32x16& sc, const f32x16& dp) {
     const unsigned ta = lds_at(team.tile[buf][0]), tb = lds_at(team.tile[buf][1]);
     const RowMeta<ROWS>& meta = team.meta[buf];
     const float k = a.to_log2;   // raw score (after the cap, if any) -> units of log2
@@ -753,13 +752,19 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>
         }
       }
       if (part) {
-        const bool bad = meta.any_bad == stamp;
+        if (odd_values) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (meta.bad[row0 + e] == stamp) x[e] = __builtin_nanf("");
+        }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const float o = meta.order[row0 + e];
-          const bool sees = (OWN_KEYS ? own.order <= o : o <= own.order) && (!docs || meta.doc[row0 + e] == own.doc);
-          if (bad && meta.bad[row0 + e] == stamp) x[e] = __builtin_nanf("");
-          x[e] = sees ? x[e] : IM_NEG_INF;
+          x[e] = (OWN_KEYS ? own.order <= o : o <= own.order) ? x[e] : IM_NEG_INF;
+        }
+        if (docs) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = meta.doc[row0 + e] == own.doc ? x[e] : IM_NEG_INF;
         }
       }
     };
@@ -873,7 +878,7 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>
     // ---- list of the next tiles ----
     if ((int)threadIdx.x < n) {
       int t = lo + (int)threadIdx.x, j = 0, len = 0, g = 0;
-      for (; j < a.n_seg; ++j) {
+      for (; j < a.str_groups; ++j) {
         if (!((live >> j) & 1u)) continue;
         len = stream_len(j);
         const int nt = (len + ROWS - 1) / ROWS, all = OWN_KEYS ? nt * a.G : nt;
@@ -883,9 +888,9 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>
         }
         t -= all;
       }
-      const int row0 = (OWN_KEYS ? a.q_off[j] : a.k_off[j]) + t * ROWS, rows = min(ROWS, len - t * ROWS);
+      const int row0 = a.str_row0[j] + t * ROWS, rows = min(ROWS, len - t * ROWS);
       const bool full = rows == ROWS && mine.all && !scan;
-      lds.list[threadIdx.x] = make_int4(row0, rows, full ? TILE_FULL : TILE_PART, g);
+      lds.list[threadIdx.x] = make_int4(row0, rows, full ? TILE_FULL | 0xf000 : TILE_PART, g);
     }
     __syncthreads();
     if (scan) {
@@ -894,8 +899,11 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>
         const bool in = lane < e.y;
         const RowInfo info = OWN_KEYS ? query_info(a, query_raw(a, b, e.x + lane, in)) : key_info(a, prefix, key_raw(a, b, e.x + lane, in));
         const Range r = range_of(info, in, ranges);
-        const int cls = OWN_KEYS ? tile_class(mine, r, e.y == ROWS, ranges) : tile_class(r, mine, e.y == ROWS, ranges);
-        if (lane == 0) lds.list[i].z = cls;
+        // each wave's rows on their own: a wave skips what none of its rows see, or saves the comparisons
+        const Range& w = lds.own[FEW ? 0 : lane & (CORE_WAVES - 1)];
+        const int cls = OWN_KEYS ? tile_class(w, r, e.y == ROWS, ranges) : tile_class(r, w, e.y == ROWS, ranges);
+        const int skip = (int)__ballot(cls == TILE_SKIP) & 15, full = (int)__ballot(cls == TILE_FULL) & 15;
+        if (lane == 0) lds.list[i].z = (skip == 15 ? TILE_SKIP : full == 15 ? TILE_FULL : TILE_PART) | skip << 8 | full << 12;
       }
       __syncthreads();
     }
@@ -907,7 +915,7 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>
       do {
         i += step;
         e = i < n ? lds.list[i] : make_int4(0, 0, TILE_FULL, 0);
-      } while (__builtin_amdgcn_readfirstlane(e.z) == TILE_SKIP);
+      } while ((__builtin_amdgcn_readfirstlane(e.z) & 3) == TILE_SKIP);
       return make_int4(__builtin_amdgcn_readfirstlane(e.x), __builtin_amdgcn_readfirstlane(e.y), __builtin_amdgcn_readfirstlane(e.z),
                        OWN_KEYS ? __builtin_amdgcn_readfirstlane(e.w) : 0);
     };
@@ -918,26 +926,31 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>
     for (;;) {
       const int4 ahead = next();
       if (e.y) {
-        arrive(buf, e.z == TILE_PART, e.y);
+        arrive(buf, (e.z & 3) == TILE_PART, e.y);
         team_sync<FEW>();   // all waves' copies are there, and nobody reads the other buffer any more
       }
       if (BUFS == 2 && ahead.y) fetch(ahead, buf ^ 1);
       if (e.y) {
-        const bool part = e.z == TILE_PART;
         ++stamp;
-        if (part) {
+        bool odd_values = false;   // replaced by 0: the row's mark counts for every wave
+        if ((e.z & 3) == TILE_PART) {
           clean(buf);
           team_sync<FEW>();
+          odd_values = __builtin_amdgcn_readfirstlane(team.meta[buf].any_bad) == stamp;
         }
         if constexpr (BIAS && OWN_KEYS) {
           typedef const float __attribute__((address_space(4))) * const_ptr;   // (a scalar load: no wait for the copies in flight)
           tile_slope2 = ((const_ptr)(uintptr_t)a.slope)[head0 + e.w] * LOG2E;
         }
+        const int w = FEW ? 0 : wave;
+        if (!((e.z >> (8 + w)) & 1)) {
+          const bool part = odd_values || !((e.z >> (12 + w)) & 1);
 #pragma unroll
-        for (int r = 0; r < ROWS / 32; ++r) {
-          f32x16 sc, dp;
-          products(buf, 32 * r, sc, dp);
-          block(buf, 32 * r, part, sc, dp);
+          for (int r = 0; r < ROWS / 32; ++r) {
+            f32x16 sc, dp;
+            products(buf, 32 * r, sc, dp);
+            block(buf, 32 * r, part, odd_values, sc, dp);
+          }
         }
         if constexpr (FEW) team_sync<FEW>();
       }
