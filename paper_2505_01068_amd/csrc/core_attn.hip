@@ -9,21 +9,44 @@
 
 namespace imattn {
 
-// One wave a query row: o = sum over splits of 2^(m_s - m) o_s / sum of 2^(m_s - m) l_s.  Bound by latency: a few KB.
-template <class T>
+// One wave a query row: o = sum over splits of 2^(m_s - m) o_s / sum of 2^(m_s - m) l_s.  Bound by latency: a few KB.  Sixteen splits at a time:
+// every load of theirs is under way before the first is waited for; lane s holds the reference and the sum of split s.
+template <class T, bool WIDE>   // WIDE: heads of more than 64 elements, two a lane
 __global__ __launch_bounds__(256) void core_join_kernel(CoreArgs a) {
   const long rows = (long)a.B * a.H * a.Tq, row = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
   if (row >= rows) return;
-  float m = -3.402823466e38f;
-  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.part_ml[2 * (s * rows + row)]);
-  float l = 0.f, o0 = 0.f, o1 = 0.f;
-  for (int s = 0; s < a.splits; ++s) {
-    const long at = s * rows + row;
-    const float f = __builtin_amdgcn_exp2f(a.part_ml[2 * at] - m);
-    l += f * a.part_ml[2 * at + 1];
-    if (lane < a.dh) o0 += f * a.part_o[at * a.dh + lane];
-    if (lane + 64 < a.dh) o1 += f * a.part_o[at * a.dh + lane + 64];
+  constexpr int N = 16;
+  float m = -3.402823466e38f, l = 0.f, o0 = 0.f, o1 = 0.f;
+  for (int s0 = 0; s0 < a.splits; s0 += N) {
+    const int n = a.splits - s0 < N ? a.splits - s0 : N;
+    // splits and elements behind the end: the last one again, with weight 0
+    const long at = (s0 + (lane < n ? lane : n - 1)) * rows + row;
+    float ms = a.part_ml[2 * at], ls = a.part_ml[2 * at + 1], v0[N], v1[WIDE ? N : 1];
+#pragma unroll
+    for (int s = 0; s < N; ++s) {
+      const float* p = a.part_o + ((s0 + (s < n ? s : n - 1)) * rows + row) * a.dh;
+      v0[s] = p[lane < a.dh ? lane : a.dh - 1];
+      if constexpr (WIDE) v1[s] = p[lane + 64 < a.dh ? lane + 64 : a.dh - 1];
+    }
+    float to = ms;
+#pragma unroll
+    for (int o = N / 2; o > 0; o >>= 1) to = fmaxf(to, __shfl_xor(to, o));
+    to = fmaxf(__shfl(to, 0), m);
+    const float before = __builtin_amdgcn_exp2f(m - to), f = lane < n ? __builtin_amdgcn_exp2f(ms - to) : 0.f;
+    m = to;
+    ls *= f;
+#pragma unroll
+    for (int o = N / 2; o > 0; o >>= 1) ls += __shfl_xor(ls, o);
+    l = l * before + __shfl(ls, 0);
+    o0 *= before;
+    o1 *= before;
+#pragma unroll
+    for (int s = 0; s < N; ++s) {
+      const float fs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), s));
+      o0 = fs == 0.f ? o0 : o0 + fs * v0[s];
+      if constexpr (WIDE) o1 = fs == 0.f ? o1 : o1 + fs * v1[s];
+    }
   }
   const float inv = l == 0.f ? 0.f : 1.f / l, lse2 = l == 0.f ? IM_NEG_INF : m + log2f(l);
   const long bh = row / a.Tq, t = row - bh * a.Tq, b = bh / a.H, head = bh - b * a.H;
@@ -274,8 +297,9 @@ int im_core_attention_fwd(const im_core_t* shape, const im_core_rules_t* rules, 
   (bf ? launch_core_fwd_bf16 : launch_core_fwd_f32)(L.few, a, L.grid, st);
   if (L.splits > 1) {
     const dim3 grid((unsigned)(((long)a.B * a.H * a.Tq + 3) / 4));
-    if (bf) hipLaunchKernelGGL(core_join_kernel<bf16_t>, grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(core_join_kernel<float>, grid, dim3(256), 0, st, a);
+    auto join = bf ? (a.dh > 64 ? core_join_kernel<bf16_t, true> : core_join_kernel<bf16_t, false>)
+                   : (a.dh > 64 ? core_join_kernel<float, true> : core_join_kernel<float, false>);
+    hipLaunchKernelGGL(join, grid, dim3(256), 0, st, a);
   }
   return after_launch(what);
 }
