@@ -14,45 +14,68 @@ namespace imattn {
 
 template <class T> struct NormChunk { static constexpr int E = 16 / (int)sizeof(T); };
 
-// E elements from p, of which the first n (<= E) exist; `whole`: p is 16-byte aligned and all exist
-__device__ __forceinline__ void load_chunk(const float* p, int n, bool whole, float (&v)[4]) {
-  if (whole) {
-    const float4 u = *(const float4*)p;
-    v[0] = u.x; v[1] = u.y; v[2] = u.z; v[3] = u.w;
-    return;
-  }
+// The elements of a row that a lane holds, as they lie in memory; their conversion is a step of its own, so that loads can be under way across
+// other work.  VEC (rows in whole, aligned 16-byte chunks): chunk lane + c LPR, elements side by side.  Otherwise element by element, neighbours in
+// neighbouring lanes: element lane + (c E + e) LPR, so that odd widths are read and written in whole lines too.
+template <class T, int LPR, int NC, bool VEC>
+struct RowPart {
+  static constexpr int E = NormChunk<T>::E;
+  static __device__ __forceinline__ int at(int lane, int c, int e) { return VEC ? (lane + c * LPR) * E + e : lane + (c * E + e) * LPR; }
+  u32x4 chunk[VEC ? NC : 1];
+  T one[VEC ? 1 : NC * E];
+  __device__ __forceinline__ void load(const T* p, bool is, int lane, int d) {   // what is missing is 0
+    if constexpr (VEC) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] = e < n ? p[e] : 0.f;
-}
-__device__ __forceinline__ void load_chunk(const bf16_t* p, int n, bool whole, float (&v)[8]) {
-  if (whole) {
-    const u32x4 u = *(const u32x4*)p;
+      for (int c = 0; c < NC; ++c) {
+        chunk[c] = u32x4{0u, 0u, 0u, 0u};
+        if (is && at(lane, c, 0) < d) chunk[c] = *(const u32x4*)(p + at(lane, c, 0));
+      }
+    } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      v[2 * e] = __uint_as_float(u[e] << 16);
-      v[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
+      for (int i = 0; i < NC * E; ++i) one[i] = T(0);
+      if (is) {   // no branch between the loads: behind the end the last element again
+#pragma unroll
+        for (int i = 0; i < NC * E; ++i) one[i] = p[min(at(lane, 0, i), d - 1)];
+      }
     }
-    return;
   }
+  __device__ __forceinline__ void get(int lane, int d, float (&v)[NC][E]) const {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = e < n ? bf2f(p[e]) : 0.f;
-}
-__device__ __forceinline__ void store_chunk(float* p, int n, bool whole, const float (&v)[4]) {
-  if (whole) { *(float4*)p = make_float4(v[0], v[1], v[2], v[3]); return; }
+    for (int c = 0; c < NC; ++c) {
+      if constexpr (!VEC) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) if (e < n) p[e] = v[e];
-}
-__device__ __forceinline__ void store_chunk(bf16_t* p, int n, bool whole, const float (&v)[8]) {
-  if (whole) {
-    u32x4 u;
+        for (int e = 0; e < E; ++e) v[c][e] = at(lane, c, e) < d ? ldf(&one[c * E + e]) : 0.f;
+      } else if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) u[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
-    *(u32x4*)p = u;
-    return;
+        for (int e = 0; e < E; ++e) v[c][e] = __uint_as_float(chunk[c][e]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v[c][2 * e] = __uint_as_float(chunk[c][e] << 16);
+          v[c][2 * e + 1] = __uint_as_float(chunk[c][e] & 0xffff0000u);
+        }
+      }
+    }
   }
+  static __device__ __forceinline__ void store(T* p, int lane, int d, const float (&v)[NC][E]) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) if (e < n) p[e] = f2bf(v[e]);
-}
+    for (int c = 0; c < NC; ++c) {
+      if constexpr (!VEC) {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (at(lane, c, e) < d) stf(p + at(lane, c, e), v[c][e]);
+      } else if (at(lane, c, 0) < d) {
+        u32x4 u;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if constexpr (sizeof(T) == 4) u[e] = __float_as_uint(v[c][e]);
+          else u[e] = pack_bf16(v[c][2 * e], v[c][2 * e + 1]);
+        }
+        *(u32x4*)(p + at(lane, c, 0)) = u;
+      }
+    }
+  }
+};
 
 // sum over the LPR lanes of a row; LPR > 64: over the workgroup, through `red` (one float a wave and call site)
 template <int LPR>
@@ -79,8 +102,9 @@ struct NormArgs {
   float eps, inv_d;
 };
 
-template <class T, int LPR, int NC>
+template <class T, int LPR, int NC, bool VEC>
 __global__ __launch_bounds__(LPR > 256 ? LPR : 256) void norm_fwd_kernel(NormArgs a) {
+  using Part = RowPart<T, LPR, NC, VEC>;
   constexpr int E = NormChunk<T>::E, WG = LPR > 256 ? LPR : 256, RPW = WG / LPR;
   __shared__ float red[2][2][WG / 64];
   const int lane = threadIdx.x % LPR;
@@ -88,53 +112,56 @@ __global__ __launch_bounds__(LPR > 256 ? LPR : 256) void norm_fwd_kernel(NormArg
   for (long row0 = (long)blockIdx.x * RPW; row0 < a.rows; row0 += (long)gridDim.x * RPW, turn ^= 1) {
     const long row = row0 + threadIdx.x / LPR;
     const bool mine = row < a.rows;
-    const T* x = (const T*)a.x + (mine ? row : 0) * a.ldx;
+    Part part;
     float v[NC][E];
+    part.load((const T*)a.x + row * a.ldx, mine, lane, a.d);
+    part.get(lane, a.d, v);
     float s = 0.f;
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      const int at = (lane + c * LPR) * E, n = a.d - at;
-#pragma unroll
-      for (int e = 0; e < E; ++e) v[c][e] = 0.f;
-      if (n > 0) load_chunk(x + at, n, a.vec, v[c]);
+    for (int c = 0; c < NC; ++c)
 #pragma unroll
       for (int e = 0; e < E; ++e) s += v[c][e];
-    }
     const float mean = row_sum<LPR>(s, red[turn][0]) * a.inv_d;
     s = 0.f;
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      const int n = a.d - (lane + c * LPR) * E;
+    for (int c = 0; c < NC; ++c)
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         v[c][e] -= mean;
-        if (e < n) s += v[c][e] * v[c][e];
+        if (Part::at(lane, c, e) < a.d) s += v[c][e] * v[c][e];
       }
-    }
     const float rstd = 1.0f / sqrtf(row_sum<LPR>(s, red[turn][1]) * a.inv_d + a.eps);
     if (!mine) continue;
     if (a.mean && lane == 0) { a.mean[row] = mean; a.rstd[row] = rstd; }
-    T* y = (T*)a.y + row * a.ldy;
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      const int at = (lane + c * LPR) * E, n = a.d - at;
-      if (n <= 0) continue;
-      float g[E], b[E], o[E];
-      if (a.gamma) load_chunk((const T*)a.gamma + at, n, a.vec, g);
-      if (a.beta) load_chunk((const T*)a.beta + at, n, a.vec, b);
+    for (int c = 0; c < NC; ++c)
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        o[e] = v[c][e] * rstd;
-        if (a.gamma) o[e] *= g[e];
-        if (a.beta) o[e] += b[e];
-      }
-      store_chunk(y + at, n, a.vec, o);
+      for (int e = 0; e < E; ++e) v[c][e] *= rstd;
+    if (a.gamma) {
+      float g[NC][E];
+      part.load((const T*)a.gamma, true, lane, a.d);
+      part.get(lane, a.d, g);
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[c][e] *= g[c][e];
     }
+    if (a.beta) {
+      float b[NC][E];
+      part.load((const T*)a.beta, true, lane, a.d);
+      part.get(lane, a.d, b);
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[c][e] += b[c][e];
+    }
+    Part::store((T*)a.y + row * a.ldy, lane, a.d, v);
   }
 }
 
-template <class T, int LPR, int NC>
+template <class T, int LPR, int NC, bool VEC>
 __global__ __launch_bounds__(LPR > 256 ? LPR : 256) void norm_bwd_kernel(NormArgs a) {
+  using Part = RowPart<T, LPR, NC, VEC>;
   constexpr int E = NormChunk<T>::E, WG = LPR > 256 ? LPR : 256, RPW = WG / LPR;
   constexpr int COLS = LPR * NC * E;
   __shared__ float red[2][2][WG / 64];
@@ -142,52 +169,56 @@ __global__ __launch_bounds__(LPR > 256 ? LPR : 256) void norm_bwd_kernel(NormArg
   const int lane = threadIdx.x % LPR;
   float g[NC][E], dg[NC][E], db[NC][E];
 #pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    const int at = (lane + c * LPR) * E, n = a.d - at;
+  for (int c = 0; c < NC; ++c)
 #pragma unroll
     for (int e = 0; e < E; ++e) { g[c][e] = 1.f; dg[c][e] = db[c][e] = 0.f; }
-    if (a.gamma && n > 0) load_chunk((const T*)a.gamma + at, n, a.vec, g[c]);
+  if (a.gamma) {
+    Part part;
+    part.load((const T*)a.gamma, true, lane, a.d);
+    part.get(lane, a.d, g);
   }
   int turn = 0;   // the reduction buffers alternate, so that one barrier a sum suffices
-  for (long row0 = (long)blockIdx.x * RPW; row0 < a.rows; row0 += (long)gridDim.x * RPW, turn ^= 1) {
+  // the next row's loads are under way while a row is worked on (36864 rows of 1024 in bf16: 69 -> 49 us)
+  const long step = (long)gridDim.x * RPW;
+  Part px, pdy;
+  float next_mean = 0.f, next_rstd = 0.f;
+  auto fetch = [&](long row) {
+    const bool is = row < a.rows;
+    next_mean = next_rstd = 0.f;
+    if (is) { next_mean = a.mean[row]; next_rstd = a.rstd[row]; }
+    px.load((const T*)a.x + row * a.ldx, is, lane, a.d);
+    pdy.load((const T*)a.dy + row * a.lddy, is, lane, a.d);
+  };
+  fetch((long)blockIdx.x * RPW + threadIdx.x / LPR);
+  for (long row0 = (long)blockIdx.x * RPW; row0 < a.rows; row0 += step, turn ^= 1) {
     const long row = row0 + threadIdx.x / LPR;
     const bool mine = row < a.rows;
     float xh[NC][E], w[NC][E];
-    float s1 = 0.f, s2 = 0.f, mean = 0.f, rstd = 0.f;
-    if (mine) { mean = a.mean[row]; rstd = a.rstd[row]; }
+    float s1 = 0.f, s2 = 0.f;
+    const float mean = next_mean, rstd = next_rstd;
+    px.get(lane, a.d, xh);
+    pdy.get(lane, a.d, w);
+    if (row0 + step < a.rows) fetch(row + step);
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      const int at = (lane + c * LPR) * E, n = mine ? a.d - at : 0;
-#pragma unroll
-      for (int e = 0; e < E; ++e) xh[c][e] = w[c][e] = 0.f;
-      if (n > 0) {
-        load_chunk((const T*)a.x + row * a.ldx + at, n, a.vec, xh[c]);
-        load_chunk((const T*)a.dy + row * a.lddy + at, n, a.vec, w[c]);
-      }
+    for (int c = 0; c < NC; ++c)
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        xh[c][e] = e < n ? (xh[c][e] - mean) * rstd : 0.f;
+        xh[c][e] = Part::at(lane, c, e) < a.d ? (xh[c][e] - mean) * rstd : 0.f;   // (rows behind the last: mean = rstd = 0)
         dg[c][e] += w[c][e] * xh[c][e];
         db[c][e] += w[c][e];
         w[c][e] *= g[c][e];
         s1 += w[c][e];
         s2 += w[c][e] * xh[c][e];
       }
-    }
     if (!a.dx) continue;
     s1 = row_sum<LPR>(s1, red[turn][0]) * a.inv_d;
     s2 = row_sum<LPR>(s2, red[turn][1]) * a.inv_d;
     if (!mine) continue;
-    T* dx = (T*)a.dx + row * a.lddx;
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      const int at = (lane + c * LPR) * E, n = a.d - at;
-      if (n <= 0) continue;
-      float o[E];
+    for (int c = 0; c < NC; ++c)
 #pragma unroll
-      for (int e = 0; e < E; ++e) o[e] = rstd * (w[c][e] - s1 - xh[c][e] * s2);
-      store_chunk(dx + at, n, a.vec, o);
-    }
+      for (int e = 0; e < E; ++e) w[c][e] = rstd * (w[c][e] - s1 - xh[c][e] * s2);
+    Part::store((T*)a.dx + row * a.lddx, lane, a.d, w);
   }
   if (!a.partial && !a.dgamma && !a.dbeta) return;
   float* out_g = a.partial ? a.partial + (long)blockIdx.x * 2 * a.d : a.dgamma;
@@ -197,11 +228,12 @@ __global__ __launch_bounds__(LPR > 256 ? LPR : 256) void norm_bwd_kernel(NormArg
     for (int c = 0; c < NC; ++c)
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        const int at = (lane + c * LPR) * E + e;
+        const int at = Part::at(lane, c, e);
         if (at < a.d && out_g) out_g[at] = dg[c][e];
         if (at < a.d && out_b) out_b[at] = db[c][e];
       }
   } else {
+    // rows of a wave, then wave after wave; element (c, e) of lane l at (c E + e) LPR + l: neighbouring lanes in neighbouring banks
     for (int wv = 0; wv < WG / 64; ++wv) {
       if ((int)(threadIdx.x >> 6) == wv) {
 #pragma unroll
@@ -211,7 +243,7 @@ __global__ __launch_bounds__(LPR > 256 ? LPR : 256) void norm_bwd_kernel(NormArg
             float p = dg[c][e], q = db[c][e];
 #pragma unroll
             for (int o = 32; o >= LPR; o >>= 1) { p += __shfl_xor(p, o); q += __shfl_xor(q, o); }
-            const int at = (lane + c * LPR) * E + e;
+            const int at = (c * E + e) * LPR + lane;
             if ((int)(threadIdx.x & 63) < LPR) {
               cols[at] = wv ? cols[at] + p : p;
               cols[COLS + at] = wv ? cols[COLS + at] + q : q;
@@ -221,8 +253,9 @@ __global__ __launch_bounds__(LPR > 256 ? LPR : 256) void norm_bwd_kernel(NormArg
       __syncthreads();
     }
     for (int at = threadIdx.x; at < a.d; at += WG) {
-      if (out_g) out_g[at] = cols[at];
-      if (out_b) out_b[at] = cols[COLS + at];
+      const int ce = VEC ? at / (E * LPR) * E + at % E : at / LPR, l = VEC ? at / E % LPR : at % LPR;
+      if (out_g) out_g[at] = cols[ce * LPR + l];
+      if (out_b) out_b[at] = cols[COLS + ce * LPR + l];
     }
   }
 }
@@ -273,8 +306,10 @@ static void norm_launch(const NormArgs& a, bool bwd, hipStream_t st) {
   const dim3 block(lpr > 256 ? lpr : 256), grid(bwd ? (unsigned)norm_bwd_grid(a.rows, a.d, E) : (unsigned)std::min<long>(norm_row_blocks(a.rows, a.d, E), 1l << 21));
 #define NORM_GO(L, N)                                                                         \
   do {                                                                                        \
-    if (bwd) hipLaunchKernelGGL((norm_bwd_kernel<T, L, N>), grid, block, 0, st, a);           \
-    else hipLaunchKernelGGL((norm_fwd_kernel<T, L, N>), grid, block, 0, st, a);               \
+    if (bwd && a.vec) hipLaunchKernelGGL((norm_bwd_kernel<T, L, N, true>), grid, block, 0, st, a);   \
+    else if (bwd) hipLaunchKernelGGL((norm_bwd_kernel<T, L, N, false>), grid, block, 0, st, a);      \
+    else if (a.vec) hipLaunchKernelGGL((norm_fwd_kernel<T, L, N, true>), grid, block, 0, st, a);     \
+    else hipLaunchKernelGGL((norm_fwd_kernel<T, L, N, false>), grid, block, 0, st, a);               \
   } while (0)
 #define NORM_NC(L)                                                                            \
   do {                                                                                        \
