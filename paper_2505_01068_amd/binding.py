@@ -413,7 +413,7 @@ def im_layernorm_fwd(x, gamma=None, beta=None, eps=1e-5, y=None, mean=None, rstd
         y = torch.empty_like(x)
     elif y.get_device() != dev:
         raise ValueError(f"{what}: y is on {y.device}, not on cuda:{dev}")
-    d, dt = x.shape[-1], x.dtype
+    d, dt = x.shape[-1] if x.dim() else 0, x.dtype
     rows, ldx = _rows(what, "x", x, d, dt)
     _, ldy = _rows(what, "y", y, d, dt, rows)
     _check((_lib or lib()).im_layernorm_fwd(rows, d, _dtype(dt), x.data_ptr(), ldx, _want(what, "gamma", gamma, (d,), dt, dev),
@@ -428,7 +428,7 @@ def im_layernorm_bwd(x, gamma, mean, rstd, dy, dx=None, dgamma=None, dbeta=None,
     dev = _device(what, x)
     if dy.get_device() != dev or (dx is not None and dx.get_device() != dev):
         raise ValueError(f"{what}: dy and dx must be on cuda:{dev}")
-    d, dt = x.shape[-1], x.dtype
+    d, dt = x.shape[-1] if x.dim() else 0, x.dtype
     rows, ldx = _rows(what, "x", x, d, dt)
     _, lddy = _rows(what, "dy", dy, d, dt, rows)
     lddx = _rows(what, "dx", dx, d, dt, rows)[1] if dx is not None else 0
@@ -494,6 +494,8 @@ def make_core(batch, q_len, k_len, n_heads, n_kv_heads, head_dim, live_mask, sca
     s.batch, s.n_seg, s.n_heads, s.n_kv_heads, s.head_dim = int(batch), len(q_len), int(n_heads), int(n_kv_heads), int(head_dim)
     for i, (nq, nk) in enumerate(zip(q_len, k_len)):
         s.q_len[i], s.k_len[i] = int(nq), int(nk)
+    if not 0 <= int(live_mask) < 1 << 64:
+        raise ValueError(f"live_mask must have at most 64 bits, got {live_mask:#x}")
     s.live_mask, s.scale, s.cap, s.causal, s.dtype = int(live_mask), float(scale), float(cap), bool(causal), _dtype(dtype)
     return s
 

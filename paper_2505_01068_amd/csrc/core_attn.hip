@@ -292,6 +292,7 @@ int im_core_attention_fwd(const im_core_t* shape, const im_core_rules_t* rules, 
   a.part_o = (float*)workspace; a.part_ml = (float*)((char*)workspace + z.part_o);
   const CoreLaunch L = core_launch(shape, false, true, a.valid_len != nullptr, a.causal || a.q_doc, &a);
   if (!L.grid) return IM_OK;
+  if (L.grid == 0xffffffffu) return refuse(IM_ERR_INVALID, "%s: problem too large (2^24 workgroups or more)", what);
   hipStream_t st = (hipStream_t)hip_stream;
   ProfScope ps(PF_ATTN_FWD, st);
   (bf ? launch_core_fwd_bf16 : launch_core_fwd_f32)(L.few, a, L.grid, st);
@@ -335,14 +336,16 @@ int im_core_attention_bwd(const im_core_t* shape, const im_core_rules_t* rules, 
   a.delta = (float*)workspace;
   a.dslope_rows = dslope ? (float*)((char*)workspace + z.stat) : nullptr;
   hipStream_t st = (hipStream_t)hip_stream;
-  const CoreLaunch Lq = core_launch(shape, false, false, a.valid_len != nullptr, a.causal || a.q_doc, &a);
+  const bool lengths = a.valid_len != nullptr, sparse = a.causal || a.q_doc;
+  const CoreLaunch Lk = core_launch(shape, true, false, lengths, sparse, nullptr), Lq = core_launch(shape, false, false, lengths, sparse, &a);
+  if (Lq.grid == 0xffffffffu || Lk.grid == 0xffffffffu) return refuse(IM_ERR_INVALID, "%s: problem too large (2^24 workgroups or more)", what);
   if (Lq.grid) {
     ProfScope ps(PF_ATTN_DQ, st);
     (bf ? launch_core_dq_bf16 : launch_core_dq_f32)(Lq.few, a, Lq.grid, st);
   }
   if (dslope) hipLaunchKernelGGL(core_dslope_kernel, dim3(a.H), dim3(1024), 0, st, a.dslope_rows, a.B, a.H, a.Tq, dslope);
-  const CoreLaunch Lk = core_launch(shape, true, false, a.valid_len != nullptr, a.causal || a.q_doc, &a);
   if (Lk.grid) {
+    core_launch(shape, true, false, lengths, sparse, &a);
     ProfScope ps(PF_ATTN_DKV, st);
     (bf ? launch_core_dkv_bf16 : launch_core_dkv_f32)(Lk.few, a, Lk.grid, st);
   }

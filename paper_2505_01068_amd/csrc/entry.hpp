@@ -32,6 +32,14 @@ inline int check_view(const char* what, const char* name, const im_view_t* v, co
   return IM_OK;
 }
 
+// An output that starts where its input does has to be the same view: elements are read and written in no particular order.
+inline int check_in_place(const char* what, const char* name, const im_view_t& in, const im_view_t& out, const int64_t (&n)[3]) {
+  if (in.ptr != out.ptr || n[0] == 0 || n[1] == 0 || n[2] == 0) return IM_OK;
+  if ((n[0] > 1 && in.batch != out.batch) || (n[1] > 1 && in.row != out.row) || (n[2] > 1 && in.head != out.head))
+    return refuse(IM_ERR_INVALID, "%s: %s in place, the strides must be the same", what, name);
+  return IM_OK;
+}
+
 // whether every head of the view starts on a multiple of `unit` bytes and is whole units long
 inline bool view_in_units(const im_view_t& v, int head_dim, size_t es, size_t unit) {
   return (uintptr_t)v.ptr % unit == 0 && head_dim * es % unit == 0 && v.batch * es % unit == 0 && v.row * es % unit == 0 && v.head * es % unit == 0;

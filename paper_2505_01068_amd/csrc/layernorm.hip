@@ -372,6 +372,7 @@ int im_layernorm_fwd(int64_t rows, int32_t d, int32_t dtype, const void* x, int6
   const size_t es = dtype == IM_DTYPE_BF16 ? 2 : 4;
   if (int rc = norm_rows_check(what, "x", x, ldx, rows, d, es)) return rc;
   if (int rc = norm_rows_check(what, "y", y, ldy, rows, d, es)) return rc;
+  if (x == y && rows > 1 && ldx != ldy) return refuse(IM_ERR_INVALID, "%s: in place, the row distances of x and y must be the same", what);
   if (!(eps > 0.f) || eps > 3e38f) return refuse(IM_ERR_INVALID, "%s: eps must be finite and > 0", what);
   if (!mean != !rstd) return refuse(IM_ERR_INVALID, "%s: mean and rstd: both or neither", what);
   if (((uintptr_t)gamma | (uintptr_t)beta) % es) return refuse(IM_ERR_INVALID, "%s: gamma or beta is not aligned to its elements", what);
@@ -397,6 +398,7 @@ int im_layernorm_bwd(int64_t rows, int32_t d, int32_t dtype, const void* x, int6
   if (int rc = norm_rows_check(what, "dy", dy, lddy, rows, d, es)) return rc;
   if (!dx && !dgamma && !dbeta) return refuse(IM_ERR_INVALID, "%s: dx, dgamma and dbeta are all NULL", what);
   if (dx) if (int rc = norm_rows_check(what, "dx", dx, lddx, rows, d, es)) return rc;
+  if (dx && dx == dy && rows > 1 && lddx != lddy) return refuse(IM_ERR_INVALID, "%s: in place, the row distances of dy and dx must be the same", what);
   if (rows > 0 && (!mean || !rstd)) return refuse(IM_ERR_INVALID, "%s: mean and rstd of the forward are needed", what);
   if ((uintptr_t)gamma % es) return refuse(IM_ERR_INVALID, "%s: gamma is not aligned to its elements", what);
   const int grid = norm_bwd_grid(rows, d, dtype == IM_DTYPE_BF16 ? 8 : 4);

@@ -173,9 +173,11 @@ extern "C" int im_rotary_apply(const im_rotary_t* s, const float* pos, int64_t p
   const int64_t nq[3] = {s->batch, s->rows, s->q_heads}, nk[3] = {s->batch, s->rows, s->k_heads};
   if (int rc = check_view(what, "q", q, nq, es, false)) return rc;
   if (int rc = check_view(what, "q_out", q_out, nq, es, true)) return rc;
+  if (int rc = check_in_place(what, "q", *q, *q_out, nq)) return rc;
   if (s->k_heads) {
     if (int rc = check_view(what, "k", k, nk, es, false)) return rc;
     if (int rc = check_view(what, "k_out", k_out, nk, es, true)) return rc;
+    if (int rc = check_in_place(what, "k", *k, *k_out, nk)) return rc;
   }
   a.rows_total = (long)s->batch * s->rows;
   if (a.rows_total == 0) return IM_OK;

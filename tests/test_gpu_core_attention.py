@@ -316,3 +316,62 @@ def test_the_same_bits_again_and_in_two_graphs(dtype, few):
                 assert torch.equal(o[n], t), (rep, n)
         for n, t in again.items():
             assert torch.equal(t, first[rep % 2][n]), (rep, n)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("rules", range(len(RULES)))
+@pytest.mark.parametrize("few", [True, False])
+def test_eight_segments(dtype, rules, few):
+    """Any block pattern over the most segments: neighbours with the same partners, with others, empty ones."""
+    print("core segments", dtype, rules, few, flush=True)
+    ql = (3, 1, 0, 33, 20, 20, 64, 5) if few else (130, 1, 0, 128, 40, 200, 64, 129)
+    kl = (40, 7, 9, 0, 64, 31, 1, 2)
+    mask = sum(row << (8 * i) for i, row in enumerate((0x35, 0x35, 0xFF, 0x00, 0xC3, 0xC3, 0xC3, 0x80)))
+    check(Case(dtype, 2, ql, kl, 4 if few else 16, 2 if few else 16, 24, mask, seed=70 + rules, **RULES[rules]))
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("cap,causal,docs", [(0.0, True, 0), (3.0, True, 4), (0.0, False, 4)])
+def test_positions_and_documents_in_any_order(dtype, cap, causal, docs):
+    """Times that run backwards or jump, document numbers up to the type's ends, slopes of both signs."""
+    print("core order", dtype, cap, causal, docs, flush=True)
+    case = Case(dtype, 2, (70, 40), (90, 160), 4, 2, 16, DENSE & 0xF, cap=cap, bias=True, causal=causal, docs=docs, seed=91)
+    g = torch.Generator().manual_seed(92)
+    for name in ("q_pos", "k_pos", "q_doc", "k_doc"):
+        t = case.rules[name]
+        if t is not None:
+            t = torch.gather(t.cpu(), 1, torch.rand(t.shape, generator=g).argsort(1))
+            if t.dtype == torch.int32:
+                t = torch.tensor([-(1 << 31), -1, 0, (1 << 31) - 1], dtype=torch.int32)[t.long()]
+            else:
+                t = t - 4.0
+            case.rules[name] = t.contiguous().cuda()
+    case.rules["slope"] = torch.tensor([0.25, -0.25, 0.0, 1.0], device="cuda")
+    check(case)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("cap", [0.0, 4.0])
+def test_a_scale_of_zero_is_the_mean(dtype, cap):
+    case = Case(dtype, 2, (40,), (70,), 2, 1, 16, 1, cap=cap, pad="key_pad", seed=5)
+    case.scale = 0.0
+    case.core = B.make_core(case.batch, case.q_len, case.k_len, 2, 1, 16, 1, 0.0, dtype, cap=cap)
+    check(case)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_two_calls_at_once(dtype):
+    """Calls on two streams, each with its own workspace, give what they give one after the other."""
+    cases = [Case(dtype, 1, (4,), (9000,), 4, 2, 64, 1, cap=8.0, seed=3), Case(dtype, 2, (200,), (300,), 4, 2, 64, 1, bias=True, seed=4)]
+    want = [{n: t.clone() for n, t in c.run().items()} for c in cases]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = []
+    for s, c in zip(streams, cases):
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            got.append(c.run())
+    torch.cuda.synchronize()
+    for a, b in zip(want, got):
+        for n in a:
+            assert torch.equal(a[n], b[n]), n

@@ -143,3 +143,20 @@ def test_the_binding_takes_tensors_of_the_current_gpu_only():
         B._dtype(torch.float16)
     with pytest.raises(ValueError):
         core(q_len=(1,))
+
+
+def test_in_place_needs_the_same_places():
+    """An operator that writes where it reads refuses a second layout of the same memory."""
+    a = {**NORM, **dict(ldy=128)}
+    assert B.lib().im_layernorm_fwd(*a.values(), None) == -1 and "in place" in err()
+    a = {**NORM_BWD, **dict(dx=P, dy=P, lddx=128)}
+    assert B.lib().im_layernorm_bwd(*a.values(), None) == -1 and "in place" in err()
+    for q, q_out, k, k_out in ((view(), view(row=128), view(512), view(1024)), (view(), view(1024), view(512), view(512, head=32)),
+                               (view(), view(batch=8192), view(512), view(1024))):
+        assert B.lib().im_rotary_apply(C.byref(rotary()), P, 3, P, q, q_out, k, k_out, None) == -1 and "in place" in err()
+
+
+@pytest.mark.parametrize("mask", [1 << 64, -1])
+def test_block_patterns_behind_64_bits_are_refused(mask):
+    with pytest.raises(ValueError, match="live_mask"):
+        core(live_mask=mask)
