@@ -815,7 +815,9 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) { x[i][e] = fast_exp2(x[i][e]); l += x[i][e]; }
+        for (int e = 0; e < 8; ++e) x[i][e] = fast_exp2(x[i][e]);
+        // (in pairs: a row of thousands of keys is no chain of thousands of roundings)
+        l += ((x[i][0] + x[i][1]) + (x[i][2] + x[i][3])) + ((x[i][4] + x[i][5]) + (x[i][6] + x[i][7]));
         p[i] = pack_p((const T*)nullptr, x[i]);
       }
     } else {
@@ -832,12 +834,16 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>
           ds[e] = x[e] * (dp[8 * i + e] - delta);
         }
         if (BIAS && WHICH == CORE_DQ && a.dslope_rows) {
+          float s = 0.f, r = 0.f, g1 = 0.f;   // eight rows' sums first, for the same reason as in the forward
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            dslope -= ds[e] * gap[BIAS ? e : 0];
-            rest += ds[e];
-            mean_gap += x[e] * gap[BIAS ? e : 0];
+            s += ds[e] * gap[BIAS ? e : 0];
+            r += ds[e];
+            g1 += x[e] * gap[BIAS ? e : 0];
           }
+          dslope -= s;
+          rest += r;
+          mean_gap += g1;
         }
         if constexpr (CAP) {
 #pragma unroll
