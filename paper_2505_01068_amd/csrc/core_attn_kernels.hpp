@@ -393,18 +393,22 @@ __device__ __forceinline__ int tile_class(const Range& keys, const Range& querie
   return full ? TILE_FULL : TILE_PART;
 }
 
-template <class T, int ND, bool FEW> struct CoreCfg {
-  static constexpr int ROWS = FEW || (sizeof(T) == 4 && ND == 4) ? 32 : 64;   // streamed rows of a tile
+template <class T, int ND, bool FEW, CoreKernel WHICH> struct CoreCfg {
+  // bf16 dK/dV of the widest heads: the owned rows of V are kept in LDS, not in 32 registers, and tiles are smaller, so that two waves a SIMD hide
+  // each other's LDS reads (3 x 3124 steps of 4 heads of 128 with documents: 374 -> 320 us; without masks 361 -> 278 us)
+  static constexpr bool OWN_LDS = sizeof(T) == 2 && ND == 4 && WHICH == CORE_DKV;
+  static constexpr int ROWS = FEW || (ND == 4 && (sizeof(T) == 4 || OWN_LDS)) ? 32 : 64;   // streamed rows of a tile
   static constexpr int TEAM = FEW ? 64 : 64 * CORE_WAVES;           // threads that load a tile together
   static constexpr int OWN = FEW ? 32 : 32 * CORE_WAVES;            // owned rows of a workgroup
-  static constexpr int BUFS = FEW && sizeof(T) == 4 && ND == 4 ? 1 : 2;   // four teams' pairs of the widest fp32 tiles do not fit the LDS twice
+  // four teams' pairs of the widest fp32 tiles do not fit the LDS twice, those of two workgroups in bf16 neither
+  static constexpr int BUFS = FEW && ND == 4 && (sizeof(T) == 4 || OWN_LDS) ? 1 : 2;
   static constexpr int N = Tile<T, ND, ROWS>::SLOTS / TEAM;         // 16-byte units a thread and tensor
 };
 
 // LDS of one team
 template <class T, int ND, bool FEW, CoreKernel WHICH>
 struct TeamLds {
-  using C = CoreCfg<T, ND, FEW>;
+  using C = CoreCfg<T, ND, FEW, WHICH>;
   char tile[C::BUFS][2][Tile<T, ND, C::ROWS>::BYTES];   // K, V or Q, dO
   RowMeta<C::ROWS> meta[C::BUFS];
   typename std::conditional<WHICH == CORE_DKV, QueryMeta<C::ROWS>, char>::type qmeta[C::BUFS];
@@ -415,6 +419,7 @@ struct CoreLds {
   __align__(16) TeamLds<T, ND, FEW, WHICH> team[TEAMS];
   int4 list[CORE_LIST];       // first row, rows, class | waves that skip it << 8 | waves that see all of it << 12, head of the group (dK/dV)
   Range own[CORE_WAVES];
+  bf16x8 own2[CoreCfg<T, ND, FEW, WHICH>::OWN_LDS ? (FEW ? 1 : CORE_WAVES) * 2 * ND * 64 : 1];
 };
 
 // A value that the compiler takes for new here: what is made of it is made here, not kept in registers from before the loop.
@@ -470,11 +475,11 @@ __device__ __forceinline__ Place place_of(const CoreArgs& a) {
 }
 
 // ---- the kernel ----
-// Waves a SIMD that the registers are cut for.  Up to head dimension 64 three (168 registers each) but for dK/dV, whose accumulators are
-// twice as many (two: 8 x 4608 steps, dQ 407 -> 356 us with three); for wider heads two, or one where even 256 registers would spill.
+// Waves a SIMD that the registers are cut for.  Up to head dimension 64 three in bf16 (168 registers each; 8 x 4608 steps, dQ 407 -> 356 us with three
+// in place of two) but for dK/dV, whose accumulators are twice as many; two otherwise, and one for wide fp32 heads, where even 256 registers would spill.
 template <class T, int ND, CoreKernel WHICH>
 constexpr int core_waves() {
-  if (ND == 4) return sizeof(T) == 4 || WHICH == CORE_DKV ? 1 : 2;
+  if (ND == 4) return sizeof(T) == 4 ? 1 : 2;
   return WHICH == CORE_DKV || sizeof(T) == 4 ? 2 : 3;
 }
 
@@ -484,7 +489,7 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>
   constexpr int ND = W ? W : 1;
   constexpr bool NARROW = W == 0;
   static_assert(!NARROW || sizeof(T) == 4, "");
-  using C = CoreCfg<T, ND, FEW>;
+  using C = CoreCfg<T, ND, FEW, WHICH>;
   using Frag = typename CoreT<T>::Frag;
   using TL = Tile<T, ND, C::ROWS>;
   constexpr int ROWS = C::ROWS, EPC = CoreT<T>::EPC, BUFS = C::BUFS;
@@ -520,13 +525,20 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>
   const float prefix = a.prefix ? a.prefix[b] : IM_NEG_INF;
   const RowInfo own = OWN_KEYS ? key_info(a, prefix, key_raw(a, b, own_row, own_valid)) : query_info(a, query_raw(a, b, own_row, own_valid));
 
-  Frag own1[2 * ND], own2[BWD ? 2 * ND : 1];   // Q (and dO), or K and V
+  Frag own1[2 * ND], own2[BWD && !C::OWN_LDS ? 2 * ND : 1];   // Q (and dO), or K and V
   if constexpr (!OWN_KEYS) {
     own_frags<ND>(head_of<const T>(a.q, b, own_row, own_head), in_range, dh, a.vec & VEC_Q, h, own1);
     if constexpr (BWD) own_frags<ND>(head_of<const T>(a.d_o, b, own_row, own_head), in_range, dh, a.vec & VEC_DO, h, own2);
   } else {
     own_frags<ND>(head_of<const T>(a.k, b, own_row, own_head), in_range, dh, a.vec & VEC_K, h, own1);
-    own_frags<ND>(head_of<const T>(a.v, b, own_row, own_head), in_range, dh, a.vec & VEC_V, h, own2);
+    if constexpr (C::OWN_LDS) {
+      if (!FEW || wave == 0) {
+        bf16x8 f[2 * ND];
+        own_frags<ND>(head_of<const T>(a.v, b, own_row, own_head), in_range, dh, a.vec & VEC_V, h, f);
+#pragma unroll
+        for (int s = 0; s < 2 * ND; ++s) lds.own2[(wave * 2 * ND + s) * 64 + lane] = f[s];
+      }
+    } else own_frags<ND>(head_of<const T>(a.v, b, own_row, own_head), in_range, dh, a.vec & VEC_V, h, own2);
   }
   const float own_slope2 = BIAS && !OWN_KEYS && in_range ? a.slope[own_head] * LOG2E : 0.f;
 
@@ -705,6 +717,7 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>
 
   const LaneAt<T, ND, ROWS> at_lane(lane);
   float tile_slope2 = 0.f;   // of the streamed tile's head
+  const unsigned own2_at = lds_at(lds.own2) + ((FEW ? 0 : wave) * 2 * ND * 64 + lane) * 16;
   auto products = [&](int buf, int row32, f32x16& sc, f32x16& dp) {
     const unsigned ta = lds_at(team.tile[buf][0]), tb = lds_at(team.tile[buf][1]);
     sc = zero16();
@@ -715,7 +728,10 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>
       dp = zero16();
 #pragma unroll
       for (int st = 0; st < 2 * ND; ++st)
-        if (sizeof(T) == 2 || 16 * st < dh) dp = at_lane.rows(tb, row32, st, own2[st], dp, dh - 16 * st);
+        if (sizeof(T) == 2 || 16 * st < dh) {
+          if constexpr (C::OWN_LDS) dp = at_lane.rows(tb, row32, st, lds_load<bf16x8>(own2_at, st * 1024), dp, 0);
+          else dp = at_lane.rows(tb, row32, st, own2[st], dp, dh - 16 * st);
+        }
     }
   };
   auto block = [&](int buf, int row32, bool part, bool odd_values, const f32x16& sc, const f32x16& dp) {
@@ -857,6 +873,7 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>
         }
         if constexpr (WHICH == CORE_DKV) p[i] = pack_p((const T*)nullptr, x);
         q[i] = pack_p((const T*)nullptr, ds);
+        if constexpr (C::OWN_LDS) __builtin_amdgcn_sched_barrier(0);   // one half's scores at a time
       }
     }
     // the second product; for dK/dV both
