@@ -496,6 +496,7 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>
   constexpr bool OWN_KEYS = WHICH == CORE_DKV, BWD = WHICH != CORE_FWD;
   extern __shared__ __align__(16) char lds_raw[];   // (nothing but the list and the owned rows' ranges outlives the walk over the tiles)
   auto& lds = *(CoreLds<T, ND, FEW, WHICH>*)lds_raw;
+  touch_args<CoreArgs>();
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), h = lane >> 5;
   const int tt = FEW ? lane : (int)threadIdx.x;     // thread of the team
   auto& team = lds.team[FEW ? wave : 0];
@@ -1011,10 +1012,10 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>
     mean_gap += other_half(mean_gap);
   }
   if constexpr (FEW) {
-    // the four waves' parts of the same rows: through LDS to wave 0, in the order of the waves
+    // the waves' parts of the same rows: through LDS to wave 0, in the order of the waves; a wave that no tile fell to has none
     constexpr int NT = WHICH == CORE_DKV ? 2 * ND : ND;
     float* box = (float*)lds_raw;                    // [NT * 16 + 3][64], the tiles are no longer needed
-    for (int w = 1; w < CORE_WAVES; ++w) {
+    for (int w = 1; w < min(CORE_WAVES, last - first); ++w) {
       if (wave == w) {
 #pragma unroll
         for (int d = 0; d < ND; ++d)

@@ -107,6 +107,7 @@ __global__ __launch_bounds__(LPR > 256 ? LPR : 256) void norm_fwd_kernel(NormArg
   using Part = RowPart<T, LPR, NC, VEC>;
   constexpr int E = NormChunk<T>::E, WG = LPR > 256 ? LPR : 256, RPW = WG / LPR;
   __shared__ float red[2][2][WG / 64];
+  touch_args<NormArgs>();
   const int lane = threadIdx.x % LPR;
   Part pg, pb;
   if (a.gamma) pg.load((const T*)a.gamma, true, lane, a.d);
@@ -166,6 +167,7 @@ __global__ __launch_bounds__(LPR > 256 ? LPR : 256) void norm_bwd_kernel(NormArg
   constexpr int E = NormChunk<T>::E, WG = LPR > 256 ? LPR : 256, RPW = WG / LPR;
   constexpr int COLS = LPR * NC * E;
   __shared__ float red[2][2][WG / 64];
+  touch_args<NormArgs>();
   __shared__ float cols[LPR > 64 ? 1 : 2 * COLS];   // the workgroup's sums, where several waves share columns
   const int lane = threadIdx.x % LPR;
   float g[NC][E], dg[NC][E], db[NC][E];

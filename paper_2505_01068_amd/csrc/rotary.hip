@@ -64,6 +64,7 @@ __device__ __forceinline__ void rot_turn(float x0, float x1, float2 w, float& y0
 template <class T, int E, bool IL>
 __global__ __launch_bounds__(ROT_THREADS) void rotary_kernel(RotArgs a) {
   extern __shared__ float2 turn[];   // [rows_per_wg][P]
+  touch_args<RotArgs>();
   for (long row0 = (long)blockIdx.x * a.rows_per_wg; row0 < a.rows_total; row0 += (long)gridDim.x * a.rows_per_wg) {
     const int nrows = (int)(a.rows_total - row0 < a.rows_per_wg ? a.rows_total - row0 : a.rows_per_wg);
     const unsigned b0 = (unsigned)row0 / (unsigned)a.rows, t0 = (unsigned)row0 - b0 * (unsigned)a.rows;
