@@ -786,8 +786,10 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>
       }
     };
     Frag p[2], q[2];
+    float x[2][8];   // (forward)
+    bool own_heavy = false, heavy = false;
     if constexpr (WHICH == CORE_FWD) {
-      float x[2][8], none[1], gap[BIAS ? 8 : 1];
+      float none[1], gap[BIAS ? 8 : 1];
       float mx = IM_NEG_INF;
 #pragma unroll
       for (int i = 0; i < 2; ++i) scores(i, x[i], none, gap);
@@ -813,6 +815,7 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>
         const float f = by > 0.f ? fast_exp2(-by) : 1.f;   // (a first reference below 0 has nothing to scale yet)
         if (mx > most) most = 8.f;
         m += by;
+        mx -= by;
         l *= f;
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -827,6 +830,12 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>
           for (int d = 0; d < ND; ++d)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc1[d][r] *= f;
+        }
+      }
+      if constexpr (sizeof(T) == 2) {
+        if (a.o32) {   // (only a backward asks for it)
+          own_heavy = 4.f * fast_exp2(mx) > l;
+          heavy = __any(own_heavy);
         }
       }
 #pragma unroll
@@ -895,6 +904,25 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>
           else acc1[d] = at_lane.cols(ta, row32 + 16 * i, d, q[i], acc1[d]);
           if constexpr (WHICH == CORE_DKV) acc2[d] = at_lane.cols(tb, row32 + 16 * i, d, p[i], acc2[d]);
         }
+    // The backward takes sum P dP from the saved output.  Where single keys carry a row, the rounding of their probabilities would be off there as much
+    // as that of dS; so a row of which one key may be an eighth or more of what it has seen (l: its half) takes what the rounding left in a
+    // second product.  (3 x 3124 steps with documents: dQ and dK 1.49 -> 1.43 times the error of one rounding at the end, for 14 us of 620.)
+    if constexpr (WHICH == CORE_FWD && sizeof(T) == 2) {
+      if (heavy) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const u32x4 w = __builtin_bit_cast(u32x4, p[i]);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            x[i][e] -= __uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
+            x[i][e] = own_heavy ? x[i][e] : 0.f;
+          }
+          const Frag left = pack_p((const T*)nullptr, x[i]);
+#pragma unroll
+          for (int d = 0; d < ND; ++d) acc1[d] = at_lane.cols(tb, row32 + 16 * i, d, left, acc1[d]);
+        }
+      }
+    }
   };
 
   for (int lo = first; lo < last; lo += CORE_LIST) {
