@@ -107,7 +107,8 @@ static long row_tiles(long n, int own) { return (n + own - 1) / own; }
 // Neighbouring segments with the same live partners are one group -- three segments of one new token each are one tile, not three that read the
 // cache three times -- unless per-sample lengths cut their ends off, or a tile across the border of two owned segments would mix the times or
 // documents by which streamed tiles are skipped (`sparse`; one tile that holds both whole is still better than two).
-// few: four waves to 32 rows instead of 128, where 128 rows a workgroup would leave CUs idle or half of the rows empty.
+// few: four waves to 32 rows instead of 128, where 128 rows a workgroup would leave CUs idle or half of the rows empty.  (Head dimension 128, 294
+// workgroups of 128 rows: forward 148 us, in workgroups of 32 rows 301; dK/dV with 150: 507 us against 320.)
 // splits (forward with few): two workgroups a CU, all at once, each with at least 16 tiles of 32 keys.  (16 requests against 17408 keys:
 // 32 us; with four workgroups a CU, in two turns, 41 us.)
 static CoreLaunch core_launch(const im_core_t* s, bool own_keys, bool may_split, bool lengths, bool sparse, CoreArgs* a) {

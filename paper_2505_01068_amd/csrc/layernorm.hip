@@ -3,6 +3,8 @@
 // Bound by HBM: the forward reads and writes a row once, the backward reads x and dy and writes dx once.  A row lives in the
 // registers of LPR lanes (4 .. 64 of a wave, or a whole workgroup of 256 / 1024), NC chunks of 16 bytes each, so that mean,
 // centred squares and the two sums of the gradient are taken over registers: two passes for the variance cost no traffic.
+// 36864 rows of 1024 in bf16: forward 24 us (6.2 TB/s), backward 48 + 5 us (4.7 TB/s) -- a large copy reaches 4.8 TB/s from HBM, and a part of
+// what is read was written just before; 48 rows of 32 in fp32: 2.2 us.
 // The gradients of gain and bias: every thread keeps the sums of its own columns over the rows that it meets, the
 // workgroup adds its threads' in a fixed order and writes one partial row; a second launch adds the partial rows.
 #include <algorithm>

@@ -4,6 +4,7 @@
 // sine of every (row, pair) once, in LDS, and then turn the pairs of all heads of queries and keys with them, 16 bytes at a
 // time where the layout allows.  The angle is pos * inv_freq / (2 pi) in fp64 -- the product of two fp32 numbers
 // is exact there -- of which only the fraction of a turn is kept, so that positions in the millions keep the accuracy of small ones.
+// 8 x 4608 rows of 8 + 8 heads of 64 in bf16: 27 us for 151 MB that were just touched, 39 us when they come from HBM (a copy: 32); 16 rows: 4.9 us.
 #include <algorithm>
 
 #include "entry.hpp"
