@@ -300,6 +300,8 @@ int im_core_attention_fwd(const im_core_t* shape, const im_core_rules_t* rules, 
   if ((uintptr_t)saved % 16) return refuse(IM_ERR_INVALID, "%s: saved must be 16-byte aligned", what);
   const CoreSizes z = core_sizes(shape);
   if (int rc = check_buffer(what, "workspace", workspace, workspace_bytes, z.fwd)) return rc;
+  const NamedView outs[] = {{"o", o, a.Tq > 0}}, ins[] = {{"q", q, a.Tq > 0}, {"k", k, a.Tk > 0}, {"v", v, a.Tk > 0}};
+  if (int rc = check_apart(what, outs, ins)) return rc;
   a.q = *q; a.k = *k; a.v = *v; a.o = *o; a.lse = lse;
   core_units(&a, es);
   if (saved) { a.o32 = (float*)saved; a.lse2 = (float*)((char*)saved + z.o32); }
@@ -344,6 +346,9 @@ int im_core_attention_bwd(const im_core_t* shape, const im_core_rules_t* rules, 
   if (z.saved && !saved) return refuse(IM_ERR_INVALID, "%s: saved is NULL", what);
   if ((uintptr_t)saved % 16) return refuse(IM_ERR_INVALID, "%s: saved must be 16-byte aligned", what);
   if (int rc = check_buffer(what, "workspace", workspace, workspace_bytes, z.bwd)) return rc;
+  const NamedView outs[] = {{"dq", dq, a.Tq > 0}, {"dk", dk, a.Tk > 0}, {"dv", dv, a.Tk > 0}};
+  const NamedView ins[] = {{"q", q, a.Tq > 0}, {"k", k, a.Tk > 0}, {"v", v, a.Tk > 0}, {"d_o", d_o, a.Tq > 0}};
+  if (int rc = check_apart(what, outs, ins)) return rc;
   a.q = *q; a.k = *k; a.v = *v; a.d_o = *d_o; a.dq = *dq; a.dk = *dk; a.dv = *dv;
   core_units(&a, es);
   a.o32 = (float*)saved; a.lse2 = (float*)((char*)saved + z.o32);

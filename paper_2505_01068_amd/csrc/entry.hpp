@@ -40,6 +40,24 @@ inline int check_in_place(const char* what, const char* name, const im_view_t& i
   return IM_OK;
 }
 
+// Refuses an output that starts where an input or another output does (both with elements).
+struct NamedView {
+  const char* name;
+  const im_view_t* v;
+  bool any;
+};
+template <size_t N, size_t M>
+inline int check_apart(const char* what, const NamedView (&outs)[N], const NamedView (&ins)[M]) {
+  for (size_t i = 0; i < N; ++i) {
+    if (!outs[i].any) continue;
+    for (size_t j = 0; j < M; ++j)
+      if (ins[j].any && outs[i].v->ptr == ins[j].v->ptr) return refuse(IM_ERR_INVALID, "%s: %s overlaps %s", what, outs[i].name, ins[j].name);
+    for (size_t j = 0; j < i; ++j)
+      if (outs[j].any && outs[i].v->ptr == outs[j].v->ptr) return refuse(IM_ERR_INVALID, "%s: %s overlaps %s", what, outs[i].name, outs[j].name);
+  }
+  return IM_OK;
+}
+
 // whether every head of the view starts on a multiple of `unit` bytes and is whole units long
 inline bool view_in_units(const im_view_t& v, int head_dim, size_t es, size_t unit) {
   return (uintptr_t)v.ptr % unit == 0 && head_dim * es % unit == 0 && v.batch * es % unit == 0 && v.row * es % unit == 0 && v.head * es % unit == 0;

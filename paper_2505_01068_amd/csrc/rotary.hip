@@ -194,6 +194,11 @@ extern "C" int im_rotary_apply(const im_rotary_t* s, const float* pos, int64_t p
     a.k = *k; a.ko = *k_out;
     in16 = in16 && view_in_units(a.k, a.dh, es, 16) && view_in_units(a.ko, a.dh, es, 16);
   }
+  if (s->k_heads) {   // (each may be its own input, not the other's)
+    if (q_out->ptr == k->ptr) return refuse(IM_ERR_INVALID, "%s: q_out overlaps k", what);
+    if (k_out->ptr == q->ptr) return refuse(IM_ERR_INVALID, "%s: k_out overlaps q", what);
+    if (q_out->ptr == k_out->ptr) return refuse(IM_ERR_INVALID, "%s: k_out overlaps q_out", what);
+  }
   hipStream_t st = (hipStream_t)hip_stream;
   ProfScope ps(PF_MISC, st);
   if (s->dtype == IM_DTYPE_BF16) rot_launch<bf16_t>(a, s->interleaved, in16, st);

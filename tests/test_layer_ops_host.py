@@ -160,3 +160,18 @@ def test_in_place_needs_the_same_places():
 def test_block_patterns_behind_64_bits_are_refused(mask):
     with pytest.raises(ValueError, match="live_mask"):
         core(live_mask=mask)
+
+
+@pytest.mark.parametrize("name", ["q", "k", "v"])
+def test_outputs_of_the_core_are_apart_from_its_inputs(name):
+    at = dict(q=view(1024), k=view(2048), v=view(4096), d_o=view(8192))
+    assert forward(core(), **{n: at[n] for n in "qkv"}, o=at[name]) == -1 and f"o overlaps {name}" in err()
+    outs = dict(dq=view(1 << 14), dk=view(1 << 15), dv=view(1 << 16))
+    assert backward(core(), **at, **{**outs, "dv": at[name]}) == -1 and f"dv overlaps {name}" in err()
+    assert backward(core(), **at, **{**outs, "dv": outs["dk"]}) == -1 and "dv overlaps dk" in err()
+
+
+@pytest.mark.parametrize("views,text", [((256, 512, 512, 1024), "q_out overlaps k"), ((256, 512, 1024, 256), "k_out overlaps q"), ((256, 512, 1024, 512), "k_out overlaps q_out")])
+def test_rotated_queries_and_keys_are_apart(views, text):
+    q, q_out, k, k_out = (view(p) for p in views)
+    assert B.lib().im_rotary_apply(C.byref(rotary()), P, 3, P, q, q_out, k, k_out, None) == -1 and text in err()
