@@ -109,8 +109,9 @@ static long row_tiles(long n, int own) { return (n + own - 1) / own; }
 // documents by which streamed tiles are skipped (`sparse`; one tile that holds both whole is still better than two).
 // few: four waves to 32 rows instead of 128, where 128 rows a workgroup would leave CUs idle or half of the rows empty.  (Head dimension 128, 294
 // workgroups of 128 rows: forward 148 us, in workgroups of 32 rows 301; dK/dV with 150: 507 us against 320.)
-// splits (forward with few): two workgroups a CU, all at once, each with at least 16 tiles of 32 keys.  (16 requests against 17408 keys:
-// 32 us; with four workgroups a CU, in two turns, 41 us.)
+// splits (forward with few): two workgroups a CU, all at once, each with at least a tile of 32 keys for every wave.  (16 requests against 17408
+// keys: 32 us; with four workgroups a CU, in two turns, 41 us.  One request of 8 heads on 2 against 4000 keys: 15.5 us, with at least four
+// tiles a wave 18.5; four of head dimension 128 against 2048: 16.1 and 21.7.)
 static CoreLaunch core_launch(const im_core_t* s, bool own_keys, bool may_split, bool lengths, bool sparse, CoreArgs* a) {
   CoreLaunch L = {};
   const int G = own_keys ? 1 : s->n_heads / s->n_kv_heads;
@@ -146,7 +147,7 @@ static CoreLaunch core_launch(const im_core_t* s, bool own_keys, bool may_split,
   L.tiles = (int)(L.few ? t32 : t128);
   L.splits = 1;
   if (may_split && L.few && L.tiles > 0)
-    L.splits = (int)std::max<long>(1, std::min<long>(2l * cu_count() / (L.tiles * groups), most / (16 * 32)));
+    L.splits = (int)std::max<long>(1, std::min<long>(2l * cu_count() / (L.tiles * groups), most / (4 * 32)));
   const long grid = (long)L.tiles * groups * L.splits;
   L.grid = grid < (1l << 24) ? (unsigned)grid : 0xffffffffu;
   if (a) {
