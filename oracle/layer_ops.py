@@ -160,8 +160,10 @@ def core_attention(q, k, v, seen, scale, cap=0.0, slope=None, q_pos=None, k_pos=
             err["dslope"] = ((e_ds + 4 * U * np.abs(ds)) * gap).sum((0, 2, 3)) + (Tk + 8) * U * (np.abs(ds) * gap).sum((0, 2, 3)) + half_step("fp32") * np.abs(out["dslope"])
         if cap:
             f = 1 - t * t
-            # the derivative's own error: twice the tangent's, and the score's
-            e_ds = e_ds * f + np.abs(ds) * (2 * np.where(hid, 0.0, e_s) / cap + 2.0 ** -20)
+            # the derivative's own error: twice the tangent's, and the score's.  A product of x +- ex and f +- ef is off by at most
+            # ex f + |x| ef + ex ef; the last term is what is left where f and x are 0 (scores at the cap, rows of one key), and scale multiplies it
+            e_f = 2 * np.where(hid, 0.0, e_s) / cap + 2.0 ** -20
+            e_ds = e_ds * (f + e_f) + np.abs(ds) * e_f
             ds = ds * f
         e_ds = e_ds + hp * np.abs(ds) + TINY
         fold = lambda x: x.reshape(B, Hkv, G, Tk, dh).sum(2)  # noqa: E731

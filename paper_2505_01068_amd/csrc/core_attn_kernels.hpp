@@ -218,6 +218,25 @@ __device__ __forceinline__ void own_frags(const float* head, bool ok, int dh, bo
       for (int e = 0; e < 4; ++e) f[s].v[4 * i + e] = __uint_as_float(u[e]);
     }
 }
+// the fragments times a power of two
+template <int N>
+__device__ __forceinline__ void scale_frags(bf16x8 (&f)[N], float by) {
+#pragma unroll
+  for (int s = 0; s < N; ++s) {
+    const u32x4 w = __builtin_bit_cast(u32x4, f[s]);
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16) * by;
+    f[s] = pack8(v);
+  }
+}
+template <int N>
+__device__ __forceinline__ void scale_frags(F8 (&f)[N], float by) {
+#pragma unroll
+  for (int s = 0; s < N; ++s)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[s].v[e] *= by;
+}
 // this half's part of the product of an owned row's fragments with a row of dh floats (16-byte aligned if dh % 4 == 0)
 template <int ND>
 __device__ __forceinline__ float dot_frags(const bf16x8 (&f)[2 * ND], const float* row, int dh, int h) {
@@ -286,7 +305,7 @@ __device__ __forceinline__ T* head_of(const im_view_t& v, long b, long row, long
 // ---- scores ----
 // The cap, c tanh(s / c).  For |s / c| < 0.4 tanh x is x (1 + u Q(u)), u = x^2, with Q of degree 2 fitted to the smallest relative
 // error there (1.2e-7, two half steps of fp32); the raw product r = s / scale takes the place of x, its powers of scale / c are in the
-// coefficients.  That is 6 multiply-adds, where (1 - e) / (1 + e), e = exp(-2 |x|), takes an exponential and a reciprocal, each four times as
+// coefficients (the host sees to it that they are of fp32's range).  That is 6 multiply-adds, where (1 - e) / (1 + e), e = exp(-2 |x|), takes an exponential and a reciprocal, each four times as
 // long.  Scores rarely come near half of their cap, so a wave looks at its largest one first (`large`) and
 // takes the exponential only if it has to; a score gives the same bits either way.
 __device__ __forceinline__ float tanh_small(const CoreArgs& a, float r) {   // tanh(c_in r) / c_in
@@ -542,6 +561,8 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>
       }
     } else own_frags<ND>(head_of<const T>(a.v, b, own_row, own_head), in_range, dh, a.vec & VEC_V, h, own2);
   }
+  if constexpr (CAP)
+    if (a.own_scale != 1.f) scale_frags(own1, a.own_scale);
   const float own_slope2 = BIAS && !OWN_KEYS && in_range ? a.slope[own_head] * LOG2E : 0.f;
 
   float own_lse2 = 0.f, own_delta = 0.f;
