@@ -330,6 +330,12 @@ __device__ __forceinline__ void tanh_of(const CoreArgs& a, float (&x)[N], bool l
   }
 }
 
+// a b, but 0 where a is 0 whatever b is.  A masked pair has weight 0, but its other factors may be anything: products with the contents of a key that
+// nobody sees, statistics and gradients of a query that sees nothing (sums of finite values may overflow too, which no look at the tile shows).
+// One instruction, v_mul_legacy_f32; the compiler knows it as an intrinsic without a builtin.
+extern "C" __device__ float intrinsic_mul_legacy(float, float) __asm("llvm.amdgcn.fmul.legacy");
+__device__ __forceinline__ float mul0(float a, float b) { return intrinsic_mul_legacy(a, b); }
+
 // ---- streamed side ----
 enum { TILE_SKIP = 0, TILE_FULL = 1, TILE_PART = 2 };
 
@@ -879,7 +885,7 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>
           float delta = own_delta;
           if constexpr (OWN_KEYS) delta = team.qmeta[buf].delta[row0 + e];
           x[e] = fast_exp2(x[e]);
-          ds[e] = x[e] * (dp[8 * i + e] - delta);
+          ds[e] = mul0(x[e], dp[8 * i + e] - delta);
         }
         if (BIAS && WHICH == CORE_DQ && a.dslope_rows) {
           float s = 0.f, r = 0.f, g1 = 0.f;   // eight rows' sums first, for the same reason as in the forward
@@ -895,13 +901,7 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>
         }
         if constexpr (CAP) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) ds[e] *= g[e];
-        }
-        // A masked pair has x = 0.  Its other factors are finite where keys are streamed (or the owned row's results are lost anyway); an owned
-        // key that nobody sees, and the statistics of a query that does not see it, may be anything.
-        if (OWN_KEYS && part) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) ds[e] = x[e] == 0.f ? 0.f : ds[e];
+          for (int e = 0; e < 8; ++e) ds[e] = mul0(ds[e], g[e]);
         }
         if constexpr (WHICH == CORE_DKV) p[i] = pack_p((const T*)nullptr, x);
         q[i] = pack_p((const T*)nullptr, ds);

@@ -2,10 +2,12 @@
 import pytest
 import torch
 
+import oracle
 from paper_2505_01068_amd import binding as B
 from tests.test_gpu_core_attention import Case, check
 
 pytestmark = pytest.mark.gpu
+IEM = oracle.IM_IEM
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
@@ -20,3 +22,59 @@ def test_any_scale_under_a_cap(dtype, cap, scale, gain):
         case.scale = float(torch.tensor(scale))
         case.core = B.make_core(2, case.q_len, k_len, 2, 1, 16, 0b1111, scale, dtype, cap=cap)
         check(case)
+
+
+HIDDEN = [dict(), dict(cap=5.0, bias=True)]
+
+
+def partly_hidden(dtype, dh, few, **rules):
+    """Queries that see nothing and keys that nobody sees, in tiles that other rows see in part."""
+    case = Case(dtype, 2 if few else 8, (40, 70, 20), (40, 70, 20), 4 if few else 24, 2 if few else 24, dh, IEM, docs=2, pad="valid_len", seed=5, **rules)
+    case.rules["valid_len"] = torch.tensor([[40, 50, 20], [40, 30, 7]], dtype=torch.int32, device="cuda").repeat(case.batch // 2, 1)
+    case.rules["q_doc"][:, 45:60] = 9
+    return case
+
+
+def same(got, want, what):
+    for n, t in want.items():
+        assert torch.equal(got[n], t), (n, what)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("dh,few", [(16, True), (64, True), (64, False), (128, False)])
+@pytest.mark.parametrize("rules", range(len(HIDDEN)))
+def test_a_query_that_sees_nothing_may_hold_anything(dtype, dh, few, rules):
+    """Its own gradient is 0 and no other result changes a bit, whatever it and its output's gradient hold."""
+    print("core blind", dtype, dh, few, HIDDEN[rules], flush=True)
+    case = partly_hidden(dtype, dh, few, **HIDDEN[rules])
+    good = {n: t.clone() for n, t in check(case).items()}
+    blind = torch.from_numpy(~case.seen().any(2)).cuda()
+    assert blind.any() and torch.all(good["dq"][blind] == 0)
+    for name in ("d_o", "q"):
+        for bad in (float("nan"), float("inf"), 3e38):
+            tensor = getattr(case, name)
+            keep = tensor.clone()
+            tensor[blind] = bad
+            out = case.run()
+            tensor.copy_(keep)
+            same(out, good, (name, bad))
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("dh,few", [(16, True), (64, True), (64, False), (128, False)])
+@pytest.mark.parametrize("rules", range(len(HIDDEN)))
+def test_a_key_that_nobody_sees_may_hold_the_largest_numbers(dtype, dh, few, rules):
+    """Products with it overflow although its values are finite: no result changes a bit."""
+    print("core large", dtype, dh, few, HIDDEN[rules], flush=True)
+    case = partly_hidden(dtype, dh, few, **HIDDEN[rules])
+    good = {n: t.clone() for n, t in check(case).items()}
+    nobody = torch.from_numpy(~case.seen().any(1)).cuda()
+    assert nobody.any()
+    sign = torch.randn(case.k.shape, generator=torch.Generator().manual_seed(8)).sign().cuda()
+    for tensor in (case.k, case.v):
+        for bad in (torch.full_like(sign, 3e38), 3e38 * sign):
+            keep = tensor.clone()
+            tensor[nobody] = bad[nobody].to(tensor.dtype)
+            out = case.run()
+            tensor.copy_(keep)
+            same(out, good, "k" if tensor is case.k else "v")
