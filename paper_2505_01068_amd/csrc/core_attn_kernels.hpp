@@ -827,14 +827,17 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>
 #pragma unroll
           for (int e = 0; e < 8; ++e) mx = fmaxf(mx, x[i][e]);
       };
-      // A cap makes no score larger: the largest |raw score|, which is known already, bounds it.
-      constexpr bool BOUND = CAP && !BIAS;
-      if constexpr (BOUND) mx = __builtin_fmaf(top, k, -m);
+      // A cap makes no score larger: the largest |raw score|, which is known already, bounds it.  (It may be a masked pair's, so a row must not be
+      // told from its bound what it does to its own results; with a backward to come the scores' maximum is taken.)
+      const bool saving = sizeof(T) == 2 && a.o32;   // (only a backward asks for it)
+      const bool bound = CAP && !BIAS && !saving;
+      if (bound) mx = __builtin_fmaf(top, k, -m);
       else largest();
+      float own_mx = mx;   // this half's part of its row
       // A row's reference is its first block's largest score and moves only when a score exceeds it by 8: probabilities stay below
       // 2^8, and no row's bits depend on another's.
       if (__any(mx > most)) {
-        if constexpr (BOUND) {
+        if (bound) {
           mx = IM_NEG_INF;
           largest();
         }
@@ -843,7 +846,7 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>
         const float f = by > 0.f ? fast_exp2(-by) : 1.f;   // (a first reference below 0 has nothing to scale yet)
         if (mx > most) most = 8.f;
         m += by;
-        mx -= by;
+        own_mx -= by;
         l *= f;
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -861,8 +864,8 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>
         }
       }
       if constexpr (sizeof(T) == 2) {
-        if (a.o32) {   // (only a backward asks for it)
-          own_heavy = 4.f * fast_exp2(mx) > l;
+        if (saving) {
+          own_heavy = 4.f * fast_exp2(own_mx) > l;
           heavy = __any(own_heavy);
         }
       }

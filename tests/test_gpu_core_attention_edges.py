@@ -78,3 +78,25 @@ def test_a_key_that_nobody_sees_may_hold_the_largest_numbers(dtype, dh, few, rul
             out = case.run()
             tensor.copy_(keep)
             same(out, good, "k" if tensor is case.k else "v")
+
+
+@pytest.mark.parametrize("dh,few", [(16, True), (64, True), (64, False), (128, False)])
+@pytest.mark.parametrize("rules", [dict(), dict(cap=5.0), dict(cap=5.0, bias=True)])
+def test_a_bf16_row_depends_on_what_it_sees_alone(dh, few, rules):
+    """In training too: neither the numbers at masked keys nor the scores of other rows of its tile change a bit of a row's results."""
+    print("core alone", dh, few, rules, flush=True)
+    case = partly_hidden("bf16", dh, few, **rules)
+    good = {n: t.clone() for n, t in check(case).items()}
+    nobody = torch.from_numpy(~case.seen().any(1)).cuda()
+    keep = case.k.clone()
+    case.k[nobody] = 50.0
+    out = case.run()
+    case.k = keep
+    same(out, good, "masked keys")
+    # every fourth query's scores grow late in the stream: the references of its neighbours' wave are looked at again
+    case.q[:, ::4] *= 8.0
+    out = case.run()
+    others = torch.arange(130, device="cuda") % 4 > 0
+    for n in ("o", "dq"):
+        assert torch.equal(out[n][:, others], good[n][:, others]), n
+    assert torch.equal(out["lse"][:, :, others], good["lse"][:, :, others])
