@@ -379,6 +379,9 @@ def _rows(what, name, t, d, dtype, n=None):
     rows, ld = 1, 0
     for i in range(len(shape) - 2, -1, -1):
         if shape[i] != 1:
+            if shape[i] == 0:   # no rows: whatever the strides
+                rows = 0
+                break
             if rows == 1:
                 ld = stride[i]
             elif stride[i] != ld * rows:
