@@ -334,7 +334,9 @@ static void norm_launch(const NormArgs& a, bool bwd, hipStream_t st) {
     case 32: NORM_GO(32, 1); break;
     case 64: if (nc == 1) NORM_GO(64, 1); else NORM_NC(64); break;
     case 256: NORM_NC(256); break;
-    default: NORM_NC(1024); break;
+    default:   // (bf16 rows of IM_NORM_MAX_D have two chunks a lane)
+      if constexpr (2 * 1024 * E < IM_NORM_MAX_D) NORM_NC(1024);
+      else NORM_GO(1024, 2);
   }
 #undef NORM_NC
 #undef NORM_GO
