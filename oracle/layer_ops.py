@@ -103,8 +103,12 @@ def visible(B, q_len, k_len, live_mask, valid_len=None, key_pad=None, q_pos=None
     return seen
 
 
-def core_attention(q, k, v, seen, scale, cap=0.0, slope=None, q_pos=None, k_pos=None, d_o=None, dtype="fp32"):
-    """q [B, Tq, H, dh], k, v [B, Tk, Hkv, dh], seen [B, Tq, Tk] -> (values, bounds): o, lse and, given d_o, dq, dk, dv, dslope."""
+def core_attention(q, k, v, seen, scale, cap=0.0, slope=None, q_pos=None, k_pos=None, d_o=None, dtype="fp32", second=False):
+    """q [B, Tq, H, dh], k, v [B, Tk, Hkv, dh], seen [B, Tq, Tk] -> (values, bounds): o, lse and, given d_o, dq, dk, dv, dslope.
+
+    second: what rounding takes off every visible probability is known to enter the saved output too (rows of a few keys), rounded in its turn:
+    2^-16 of a probability is missing there, not 2^-8.
+    bounds["dslope_sharp"]: as dslope's bound, but with the part of dS's errors that is the same for a whole row taken back, as the kernel does."""
     q, k, v = (np.asarray(t, np.float64).transpose(0, 2, 1, 3) for t in (q, k, v))
     B, H, Tq, dh = q.shape
     Hkv, Tk = k.shape[1], k.shape[2]
@@ -152,12 +156,22 @@ def core_attention(q, k, v, seen, scale, cap=0.0, slope=None, q_pos=None, k_pos=
         dp, e_dp = do @ vt, (dh + 4) * U * (np.abs(do) @ np.abs(vt))
         delta = (do * o).sum(-1, keepdims=True)
         # the saved o is fp32, but formed from rounded probabilities
-        e_delta = (np.abs(do) * (e_o + U * np.abs(o))).sum(-1, keepdims=True) + (dh + 4) * U * (np.abs(do) * np.abs(o)).sum(-1, keepdims=True)
+        e_saved = (e_p + 2.0 ** -16 * p + 2 * (Tk + 4) * U * p) @ av if second and dtype == "bf16" else e_o
+        e_delta = (np.abs(do) * (e_saved + U * np.abs(o))).sum(-1, keepdims=True) + (dh + 4) * U * (np.abs(do) * np.abs(o)).sum(-1, keepdims=True)
         ds = p * (dp - delta)
         e_ds = e_p * np.abs(dp - delta) + p * (e_dp + e_delta) + 4 * U * np.abs(ds)
         if slope is not None:
             out["dslope"] = -(ds * gap).sum((0, 2, 3))
             err["dslope"] = ((e_ds + 4 * U * np.abs(ds)) * gap).sum((0, 2, 3)) + (Tk + 8) * U * (np.abs(ds) * gap).sum((0, 2, 3)) + half_step("fp32") * np.abs(out["dslope"])
+            # What the kernel sums is -sum (dS - R P) gap with R = sum dS, the row's sum, and G = sum P gap:  -sum dS gap + R G.  An error x of a
+            # pair's dS so counts x (gap - G), and delta's, which is P times one number for the whole row, only by what sum P misses of 1.
+            # (Tk + 10) U for each sum, its products and the distance's own rounding.
+            g_row = (p * gap).sum(-1, keepdims=True)
+            e_one = e_p * np.abs(dp - delta) + p * e_dp + 4 * U * (np.abs(ds) + p * e_delta)
+            e_rest = e_delta + e_one.sum(-1, keepdims=True)
+            pairs = e_one * np.abs(gap - g_row) + (Tk + 10) * U * (np.abs(ds) + p * e_rest) * (gap + g_row)
+            rows_left = e_rest * g_row * (e_p.sum(-1, keepdims=True) + (Tk + 10) * U)
+            err["dslope_sharp"] = pairs.sum((0, 2, 3)) + rows_left.sum((0, 2, 3)) + half_step("fp32") * np.abs(out["dslope"])
         if cap:
             f = 1 - t * t
             # the derivative's own error: twice the tangent's, and the score's.  A product of x +- ex and f +- ef is off by at most
