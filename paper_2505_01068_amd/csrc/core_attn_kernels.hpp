@@ -1032,7 +1032,12 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>
         if constexpr (FEW) team_sync<FEW>();
       }
       if (!ahead.y) break;
-      if (BUFS == 1) fetch(ahead, 0);
+      if constexpr (BUFS == 1) {
+        // a copy is no LDS instruction: what the wave still reads of the tile has to be there first (with two buffers the list's entry, read
+        // after the tile that the copies replace and in order with it, is what their addresses wait for)
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        fetch(ahead, 0);
+      }
       buf ^= BUFS - 1;
       e = ahead;
     }
