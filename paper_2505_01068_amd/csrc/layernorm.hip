@@ -382,6 +382,7 @@ int im_layernorm_fwd(int64_t rows, int32_t d, int32_t dtype, const void* x, int6
   if (!(eps > 0.f) || eps > 3e38f) return refuse(IM_ERR_INVALID, "%s: eps must be finite and > 0", what);
   if (!mean != !rstd) return refuse(IM_ERR_INVALID, "%s: mean and rstd: both or neither", what);
   if (((uintptr_t)gamma | (uintptr_t)beta) % es) return refuse(IM_ERR_INVALID, "%s: gamma or beta is not aligned to its elements", what);
+  if (((uintptr_t)mean | (uintptr_t)rstd) % 4) return refuse(IM_ERR_INVALID, "%s: mean or rstd is not aligned to its elements", what);
   if (rows == 0) return IM_OK;
   NormArgs a = {};
   a.rows = rows; a.d = d; a.x = x; a.ldx = ldx; a.gamma = gamma; a.beta = beta; a.y = y; a.ldy = ldy; a.mean = mean; a.rstd = rstd;
@@ -407,6 +408,8 @@ int im_layernorm_bwd(int64_t rows, int32_t d, int32_t dtype, const void* x, int6
   if (dx && dx == dy && rows > 1 && lddx != lddy) return refuse(IM_ERR_INVALID, "%s: in place, the row distances of dy and dx must be the same", what);
   if (rows > 0 && (!mean || !rstd)) return refuse(IM_ERR_INVALID, "%s: mean and rstd of the forward are needed", what);
   if ((uintptr_t)gamma % es) return refuse(IM_ERR_INVALID, "%s: gamma is not aligned to its elements", what);
+  if (((uintptr_t)mean | (uintptr_t)rstd | (uintptr_t)dgamma | (uintptr_t)dbeta) % 4)
+    return refuse(IM_ERR_INVALID, "%s: mean, rstd, dgamma or dbeta is not aligned to its elements", what);
   const int grid = norm_bwd_grid(rows, d, dtype == IM_DTYPE_BF16 ? 8 : 4);
   const bool sums = dgamma || dbeta;
   const size_t need = sums && grid > 1 ? round256((size_t)grid * 2 * d * sizeof(float)) : 0;
