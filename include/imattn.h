@@ -299,7 +299,7 @@ int im_layernorm_bwd(int64_t rows, int32_t d, int32_t dtype, const void* x, int6
  *   (x0, x1) -> (x0 cos - x1 sin, x0 sin + x1 cos),  inverse: by the negative angle -- the gradient of the rotation.
  * The first pairs[0] pairs belong to axis 0, the next pairs[1] to axis 1, ...; P = sum of pairs, 1 <= P <= head_dim / 2.
  * Pair p is the elements (p, P + p) of a head, or (2p, 2p + 1) with `interleaved`; elements from 2P on are copied.
- * Angles are formed and reduced in 64 bits: far positions lose nothing.
+ * Angles are formed and reduced in 64 bits: up to 5e8 radians they are off by less than 6e-8, half a step of fp32, however far the position.
  * device in : pos fp32 [batch, rows, n_axes], pos_batch elements from one batch element to the next (0: shared by all);
  *             inv_freq fp32 [P]; views q (q_heads heads) and k (k_heads heads; 0: no keys, k and k_out may be NULL).
  * device out: views q_out, k_out (may be q and k: in place, same strides).
@@ -323,7 +323,12 @@ int im_rotary_apply(const im_rotary_t* shape, const float* pos, int64_t pos_batc
  * the backward no key's that none of those queries sees.
  * n_heads is a multiple of n_kv_heads: query head h reads key head h / (n_heads / n_kv_heads).  Any head_dim from 1 to 128.
  * Queries and keys have lengths of their own (q_len, k_len: segments one after the other; 0 is allowed, also for all).
- * With few query rows (new tokens against a long cache) the keys are split over workgroups and the parts joined. */
+ * With few query rows (new tokens against a long cache) the keys are split over workgroups and the parts joined.
+ * Rounding: sums, statistics and scores are fp32.  With dtype IM_DTYPE_BF16 probabilities (and, in the backward, dS) are rounded to bf16 once where they enter
+ * the second products, beside the one rounding of a result: measured over rows of 100 to 4600 keys, o is off by 1.1 and dq, dk, dv by 1.4 times the error of
+ * that rounding alone.  With
+ * `saved` what the rounding takes off probabilities that carry a row is added in a second product, so o of a bf16 call with and without `saved` agrees to
+ * rounding, not bit for bit.  A query's results depend on what it sees alone: not on the contents of masked keys, nor on other queries. */
 typedef struct im_core {
   int32_t batch, n_seg;
   int32_t q_len[IM_MAX_SEG], k_len[IM_MAX_SEG];

@@ -123,7 +123,8 @@ def core_attention(q, k, v, seen, scale, cap=0.0, slope=None, q_pos=None, k_pos=
     if cap:
         t = np.tanh(raw / cap)
         s = cap * t
-        # |tanh'| <= 1; the function itself to 2^-21 in bf16 (see the kernel's 1 - 2 / (1 + e)), to 8 u relative in fp32
+        # |tanh'| <= 1; the function itself to 8 u relative in fp32.  bf16 takes the same polynomial and exponential; 2^-21 of the cap is more than
+        # they need (a bound in the cap, not in the score), and still far below what bf16 operands leave.
         e_s = e_s + (cap * 2.0 ** -21 if dtype == "bf16" else 8 * U * np.abs(s)) + 4 * U * np.abs(s)
     gap = None
     if slope is not None:

@@ -11,9 +11,12 @@
 // first product(s) and transposed for the second: by the LDS transpose read in bf16, by plain reads in fp32, whose
 // products run on v_mfma_f32_32x32x2_f32 (exact fp32 multiply-adds; a sixteenth of the bf16 rate).
 //
-// What bounds them: not the matrix cores but the score arithmetic.  8 x 4608 steps, 8 heads of 64, the diagonal blocks live, scores capped: 250 to
-// 300 us in the forward, 0.5 PFLOP/s, vector instructions issued in 87 % of the cycles -- about 13 a score, the softmax's exponential and its share of
-// the cap's polynomial among them.  In fp32 from head dimension 64 on the fp32 matrix rate does; for single tokens against long caches HBM (26 us for 107 MB);
+// What bounds them: not the matrix cores but the score arithmetic.  8 x 4608 steps, 8 heads of 64, the diagonal blocks live, scores capped: 590 thousand
+// cycles in the forward, 258 us, or 310 where the clock falls under sustained load; the vector units issue in 77 % of the cycles in which a CU has work --
+// 11 instructions a score, the softmax's exponential and its share of the cap's polynomial among them -- the matrix units are busy in 25 %.  Training with
+// cap and bias: vector 81 / 90 / 63 %, matrix 22 / 23 / 24 % in forward, dQ and dK/dV.  In fp32 at a head of 5 no unit is: vector 50 / 44 / 38 %, matrix
+// 27 / 27 / 36 %, segments of 50 rows leave 61 % of a 128-row tile empty; from head dimension 64 on the fp32 matrix rate bounds.  With documents
+// the waves wait for copies and each other in 57 / 62 / 64 % of their cycles.  For single tokens against long caches HBM (26 us for 107 MB);
 // for the smallest calls (9 us) the chain of loads and the instructions that are met for the first time.
 //
 // Which streamed tiles are visited is decided from the data, once per workgroup and 64 tiles: a tile in which no owned row
@@ -156,7 +159,9 @@ struct LaneAt<float, ND, ROWS> {
     return c;
   }
 };
-__device__ __forceinline__ bf16x8 pack_p(const bf16_t*, const float* p) { return pack8(p); }   // the one rounding of probabilities and dS
+// The one rounding of probabilities and dS: the second products then run at the bf16 rate.  Errors against 64 bits become 1.4 times those of a result's own
+// rounding in dq, dk and dv (0.0024 for 0.0017) and 1.1 times in o (0.0018); a second bf16 part of each would double the second products and their packing.
+__device__ __forceinline__ bf16x8 pack_p(const bf16_t*, const float* p) { return pack8(p); }
 __device__ __forceinline__ F8 pack_p(const float*, const float* p) {
   F8 f;
 #pragma unroll
