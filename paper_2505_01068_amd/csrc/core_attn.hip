@@ -217,15 +217,13 @@ static void core_args(const im_core_t* s, const im_core_rules_t* r, CoreArgs* a)
   // Below scale / cap = 1e-42 a cap changes nothing: no raw score exceeds 3.5e38, and tanh x = x (1 - x^2 / 3 + ..) to half a step of fp32
   // where x < 4e-4.
   if (a->cap != 0.f && (double)s->scale / s->cap < 1e-42) a->cap = 0.f;
-  a->own_scale = 1.f;
-  int n = 0;
+  int n = a->cap == 0.f && s->scale > 1e38f ? 2 : 0;   // (scale * log2(e) stays finite: a score of 0 is no 0 times infinity)
   if (a->cap != 0.f) {
     double c = (double)s->scale / s->cap;
     // Coefficients in the raw score hold powers of c up to the sixth.  Where those would leave fp32 the owned rows take a power of two, exactly,
     // and c is that much closer to 1.  (At most 2^32, by which rows below 2^96 stay finite; from c = 2^48 on, where raw scores of 1e-14 are at their
     // cap, every score takes the exponential.)
     if (!(c > 1e-5 && c < 1e5)) n = std::max(-126, std::min(32, ilogb(c)));
-    a->own_scale = ldexpf(1.f, n);
     c = ldexp(c, -n);
     const double c2 = c * c;
     a->c_in = (float)c;
@@ -235,6 +233,7 @@ static void core_args(const im_core_t* s, const im_core_rules_t* r, CoreArgs* a)
     const double q[3] = {-0.33331882, 0.13277628, -0.0477942};
     for (int i = 0; i < 3; ++i) a->tanh_q[i] = in ? (float)(q[i] * pow(c2, i + 1)) : 0.f;
   }
+  a->own_scale = ldexpf(1.f, n);
   a->to_log2 = ldexpf(s->scale, -n) * 1.44269504088896340736f;
   a->scale = s->scale;
   if (r) {

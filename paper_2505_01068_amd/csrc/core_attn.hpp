@@ -18,7 +18,7 @@ struct CoreArgs {
   unsigned vec, words;            // bit per tensor (VecBit): heads in aligned units of 16 bytes, of 4 bytes
   int causal;
   float cap;
-  float own_scale;                // power of two by which owned rows enter the raw score (1 but where scale / cap is extreme)
+  float own_scale;                // power of two by which owned rows enter the raw score (1 but where scale or scale / cap is extreme)
   float to_log2;                  // scale / own_scale * log2(e): raw score (after the cap) -> units of log2
   float c_in, inv_c_in;           // scale / own_scale / cap: raw score -> argument of the tangent
   float small_to, tanh_q[3];      // raw scores below small_to take the polynomial 1 + u (q0 + u (q1 + u q2)), u = raw^2

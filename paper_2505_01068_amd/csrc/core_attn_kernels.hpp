@@ -572,8 +572,7 @@ __global__ __launch_bounds__(64 * CORE_WAVES, (core_waves<T, (W ? W : 1), WHICH>
       }
     } else own_frags<ND>(head_of<const T>(a.v, b, own_row, own_head), in_range, dh, a.vec & VEC_V, h, own2);
   }
-  if constexpr (CAP)
-    if (a.own_scale != 1.f) scale_frags(own1, a.own_scale);
+  if (a.own_scale != 1.f) scale_frags(own1, a.own_scale);
   const float own_slope2 = BIAS && !OWN_KEYS && in_range ? a.slope[own_head] * LOG2E : 0.f;
 
   float own_lse2 = 0.f, own_delta = 0.f;

@@ -100,3 +100,16 @@ def test_a_bf16_row_depends_on_what_it_sees_alone(dh, few, rules):
     for n in ("o", "dq"):
         assert torch.equal(out[n][:, others], good[n][:, others]), n
     assert torch.equal(out["lse"][:, :, others], good["lse"][:, :, others])
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("scale", [1e38, 2.4e38, 3.4e38])
+def test_scores_of_zero_under_the_largest_scales(dtype, scale):
+    """Without a cap: queries of zeros see the mean of their values."""
+    print("core largest scale", dtype, scale, flush=True)
+    case = Case(dtype, 2, (33, 20), (40, 30), 2, 1, 16, 0b1111, seed=12)
+    case.scale = float(torch.tensor(scale))
+    case.core = B.make_core(2, case.q_len, case.k_len, 2, 1, 16, 0b1111, scale, dtype)
+    case.q.zero_()
+    case.d_o.zero_()   # (dq is scale times what rounding leaves of dS: nothing to hold it to)
+    check(case)
